@@ -291,7 +291,7 @@ def _vocab_plain(s, to):
     row_loss = torch.where(there, lse - z.gather(1, column)[:, 0], 0.0)
     share = s["weight"] if case["weighted"] else 1.0 / there.sum().clamp_min(1)
     share = torch.where(there, share, 0.0)
-    out = {"loss": (row_loss * share).sum()[None], "row_loss": row_loss, "lse": lse}
+    out = {"loss": (row_loss * share).sum()[None], "row_loss": row_loss, "lse": torch.where(there, lse, 0.0)}
     if case["grads"]:
         p = (e / total).scatter_add(1, column, torch.full_like(column, -1.0, dtype=torch.float32)) * share[:, None]
         out.update(dh=(p @ w).to(to), dw=(p.T @ h).to(to))
@@ -340,7 +340,7 @@ def exact(case, seed):
         row_loss = torch.zeros_like(lse)
         row_loss[there] = (lse - z[rows, s["target"].long()])[there]
         share = f["weight"] * there if case["weighted"] else there.double() / max(1, int(there.sum()))
-        out = {"loss": torch.dot(row_loss, share)[None], "row_loss": row_loss, "lse": lse}
+        out = {"loss": torch.dot(row_loss, share)[None], "row_loss": row_loss, "lse": lse * there}
         if case["grads"]:
             g = z.sub_(lse[:, None]).exp_()
             g[rows[there], s["target"].long()[there]] -= 1.0
