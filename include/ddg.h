@@ -306,6 +306,91 @@ size_t ddg_pipeline_mail_bytes(const ddg_pipeline* p, int k);
 ddg_status ddg_pipeline_get_mail(ddg_pipeline* p, int k, void* host_dst, long* iteration);
 ddg_status ddg_pipeline_set_mail(ddg_pipeline* p, int k, const void* host_src, long iteration);
 
+/* ---- operators of token models ---------------------------------------------------------------
+ * Next to the convolutional modules: what a module of a token model needs at its joins and at its
+ * end. These calls have no module: a descriptor holds the sizes and the stream, the caller owns
+ * every tensor and the workspace, nothing is allocated, waited for or kept between calls, and all
+ * of them can be captured into a graph. Rows are tokens; a tensor [rows][cols] has its columns
+ * next to each other and `ld` elements from row to row (0: as many as it has columns). Tensors
+ * are of the descriptor's dtype unless the call says otherwise; any pointer and any ld work, 16-byte
+ * pointers and rows of whole 16-byte pieces are faster. Outputs may not overlap anything else
+ * that a call reads or writes, except where it says so. dry_run != 0: only the checks.
+ * rows (tokens) may be 0. */
+
+/* Dropout: y = x * 65536/(65536-t) where the draw of (row, column) is t or more, else 0, with
+ * t = round(65536 p), 0 <= p < 1 (t at most 65535). The draws are 16-bit pieces of Philox4x32-7
+ * (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011) with key `seed` and
+ * counter (column / 8, row, step): a function of its arguments alone, so no mask is stored.
+ * The gradient is the same call on the error gradient; a module of delay K-k that re-forwards
+ * the input of iteration s passes the step of s and gets the mask of s. An element that is
+ * dropped is 0 whatever it was (infinity and NaN too). y may be x (same ld). */
+typedef struct {
+  int rows, cols, dtype;
+  float p;
+  uint64_t seed;
+  long ld_x, ld_y;
+  void* stream;
+  int dry_run;
+} ddg_dropout_desc;
+ddg_status ddg_dropout(const ddg_dropout_desc* d, uint64_t step, const void* x, void* y);
+
+/* Join of a residual branch and the norm that follows it:
+ *   x = residual + dropout(y),  rstd = (mean_c x^2 + eps)^(-1/2),  out = gain * x * rstd,
+ * cols up to 32768. residual NULL: x = dropout(y). gain: fp32 [cols], NULL: 1. x_out [rows][cols] and
+ * rstd (fp32 [rows]) are what the backward pass needs; each may be NULL. x_out may be y or
+ * residual (same ld). Sums are fp32, out comes from the unrounded x. */
+typedef struct {
+  int rows, cols, dtype;
+  float eps;                 /* > 0 */
+  float p;                   /* of the dropout; 0: none */
+  uint64_t seed;
+  long ld_y, ld_residual, ld_x, ld_out;
+  int group;                 /* 8-bit output: columns that share a scale, 128, or 0: the row */
+  void* stream;
+  int dry_run;
+} ddg_join_desc;
+ddg_status ddg_join_norm(const ddg_join_desc* d, uint64_t step, const void* y, const void* residual, const float* gain,
+                         void* x_out, void* out, float* rstd);
+/* The same with `out` in 8 bits for products of 8-bit operands: scale = max(|out| over the group) / 448
+ * (fp32 [rows][groups], at least 2^-126), q = out / scale rounded to nearest even in the e4m3
+ * format (4 exponent bits, 3 of fraction, largest value 448, no infinities), [rows][cols] bytes, ld_out. */
+ddg_status ddg_join_norm_q8(const ddg_join_desc* d, uint64_t step, const void* y, const void* residual, const float* gain,
+                            void* x_out, uint8_t* q, float* scale, float* rstd);
+/* Backward: from x and rstd of the forward pass, d_out = df/d(out) and d_x = df/d(x) through x_out
+ * (NULL: none), with xhat = x * rstd and c = mean_c(gain d_out xhat):
+ *   d_residual = d_x + rstd (gain d_out - xhat c),  d_y = dropout(d_residual),  d_gain = sum_rows d_out xhat.
+ * ld_x is of x and d_x, ld_out of d_out, ld_residual of d_residual, ld_y of d_y. Each result may be
+ * NULL (d_y where p = 0 equals d_residual). d_residual may be d_x, if ld_residual = ld_x. d_gain: fp32 [cols], rows summed
+ * in a fixed order; it needs the workspace (ddg_join_norm_workspace bytes, 16-byte aligned). */
+size_t ddg_join_norm_workspace(const ddg_join_desc* d);
+ddg_status ddg_join_norm_backward(const ddg_join_desc* d, uint64_t step, const void* x, const float* rstd, const float* gain,
+                                  const void* d_out, const void* d_x, void* d_residual, void* d_y, float* d_gain,
+                                  void* workspace, size_t workspace_bytes);
+
+/* Head of a token model: softmax cross entropy over a vocabulary, from the hidden states h
+ * [tokens][dim] and a row of w [vocab][dim] for each entry, without the logits z = h w^T in memory:
+ *   loss_i = log(sum_j exp z_ij) - z_i,target_i,   loss = sum_i a_i loss_i,
+ *   dh = P w, dw = P^T h  with  P_ij = a_i (exp(z_ij - lse_i) - [j = target_i]).
+ * targets: int32 [tokens]; a negative one means that the token has none: its loss, its lse and its
+ * row of dh are 0, and nothing in its row of h reaches dw. A target of vocab or more makes that
+ * loss NaN. weights: fp32 [tokens], the a_i; NULL: the mean over the tokens with a target (0 if there are none).
+ * loss: fp32 scalar; row_loss, lse: fp32 [tokens], unweighted; dh [tokens][dim], dw [vocab][dim] (dw_f32 != 0: in fp32 whatever the
+ * dtype). Each of the five may be NULL. Products of bf16 operands are summed in fp32; with gradients in bf16, P is
+ * rounded to bf16 (exp(z - m) before the scale by exp(m - lse), and P after it). ddg_vocab_loss_workspace: bytes
+ * of the workspace (256-byte aligned), with gradients (dh or dw) or without. It holds, besides a few words per token and the
+ * gathered rows of h, at most 1040 MiB of P (or 256 tokens' where that is more), and the fp32 sum of dw if tokens take several turns;
+ * more where h or w is not 16-byte aligned although its rows are whole pieces: the call then names the size. 0 if the descriptor is refused. */
+typedef struct {
+  int tokens, dim, vocab, dtype;
+  long ld_h, ld_w, ld_dh, ld_dw;
+  int dw_f32;
+  void* stream;
+  int dry_run;
+} ddg_vocab_desc;
+size_t ddg_vocab_loss_workspace(const ddg_vocab_desc* d, int gradients);
+ddg_status ddg_vocab_loss(const ddg_vocab_desc* d, const void* h, const void* w, const int32_t* targets, const float* weights,
+                          float* loss, float* row_loss, float* lse, void* dh, void* dw, void* workspace, size_t workspace_bytes);
+
 /* ---- measurement ----------------------------------------------------------------------------
  * Per-kernel-family timing with HIP events on the module's stream. While enabled, every launch
  * of a kernel family is bracketed by two events; ddg_profile_read synchronises and returns, for

@@ -1,0 +1,664 @@
+// Softmax cross entropy over a vocabulary without its logits. With hidden states h [T][D], vocabulary rows w [V][D] and z = h w^T,
+//   l_i = log sum_j exp z_ij - z_i,t_i,   f = sum_i a_i l_i,   P_ij = a_i (exp(z_ij - lse_i) - [j = t_i]),   dh = P w,   dw = P^T h.
+// Three matrix products of one kernel (product_kernel), a panel of tokens at a time:
+//   1. z^T = w h^T, a tile of the vocabulary by tokens. A logit lives in a register only: the tile leaves the maximum m and sum of exp(z - m)
+//      of each token over the columns of a wave, and, for gradients, exp(z - m) itself in the operands' type.
+//   2. dh^T = w^T P^T    3. dw^T = h^T P
+// and between 1 and 2 a pass that joins a token's maxima and sums and turns exp(z - m) into P in place. What is kept of the T x V values is a
+// panel's, in the operands' type, of bounded size. Tokens without a target are left out: the others are gathered first.
+#include "ddg_device.h"
+#include "ddg_token.h"
+
+namespace ddg {
+namespace {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// ---- the product ---------------------------------------------------------------------------------
+
+// out[n][m] = sum_k A(m, k) B(n, k). An operand whose rows run along k (KC) is [rows][k], one whose rows run along the tile is [k][rows].
+struct ProductArgs {
+  const void* A; const void* B;
+  long lda, ldb;
+  int M, N, K;               // K: 16-byte pieces of a KC operand start below it; the other kind's rows end there
+  const int* count;          // tokens left over the panels, or null: `dynamic` says which of N (1) and K (2) they bound
+  int first, dynamic;        // first token of the panel
+  int tiles_m, tiles_n, splits;
+  // epilogue 1: exp(z - m), maxima and sums, the target's logit
+  void* e; long lde; float2* stat; int stats; const int* target; float* zt;
+  // epilogue 2: out[map[n]][m] = scale * sum + prev
+  void* out; long ldo; int out_f32; const float* prev; long ldp; const float* scale; const int* map; size_t split_stride;
+  int vec;                   // rows of `out` are 4-element pieces
+};
+
+// 16 bytes a lane from memory straight to LDS, at `lds` + 16 * lane; lanes at NOWHERE write zeros. Nothing waits here: the load has no output register,
+// and whoever reads that LDS waits for the counter first (step_barrier).
+__device__ __forceinline__ void to_lds(u32x4 res, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(res) : "memory");
+}
+// Every load of this wave has arrived and every LDS read has been answered, in all waves
+__device__ __forceinline__ void step_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+__device__ __forceinline__ u32x4 resource(const void* p) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)a), (unsigned)__builtin_amdgcn_readfirstlane((int)((unsigned)(a >> 32) & 0xffffu)),
+               0x80000000u, 0x00027000u};
+}
+
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> {
+  typedef bf16x8_t t;
+  __device__ static __forceinline__ f32x16_t mma(t a, t b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Frag<float> {
+  typedef f32x4_t t;
+  // four instructions of k = 2: instruction j contracts element j of both half-waves
+  __device__ static __forceinline__ f32x16_t mma(t a, t b, f32x16_t c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// One operand's tile of a step in LDS: R rows of the tile by 128 bytes of k.
+//   KC: [R][128 bytes], 16-byte piece c of row r at place c ^ (r & 7): the 32 rows that a fragment read takes at one k spread over all banks.
+//   else: [BK][R], whose fragments are read transposed; 64-byte pieces (bf16: 32 columns) of row k at place piece ^ (k & 3), so that the four
+//   rows of a transposing read lie in different banks (R = 64: two rows to 256 bytes, place ^ (k >> 1 & 1)); fp32: 128-byte pieces, place ^ (k >> 2 & 1).
+template <typename T, int R, bool KC, int NT> struct Operand {
+  static constexpr int SZ = sizeof(T), BK = 128 / SZ, BYTES = R * 128, LOADS = R * 8 / NT, RB = R * SZ, PER = RB / 16;
+  static_assert(LOADS >= 1 && R * 8 % NT == 0, "every thread loads");
+  unsigned off[LOADS];       // bytes from the step's base
+  int kpos[KC ? 1 : LOADS];  // k of the loads (KC: of all)
+  const unsigned char* base;
+  long advance;
+
+  static __device__ __forceinline__ int swizzle(int k) {    // in 16-byte pieces
+    if (SZ == 4) return ((k >> 2) & 1) << 3;
+    return RB >= 256 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+  }
+  // rows [r0, r0 + R) of `rows`, from k0 on
+  __device__ __forceinline__ void init(const void* p, long ld, int r0, int rows, int k0, int tid) {
+    if (KC) {
+      base = (const unsigned char*)p + ((size_t)r0 * ld + k0) * SZ;
+      advance = 128;
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        const int r = tid / 8 + j * (NT / 8), c = (tid % 8) ^ (r & 7);
+        off[j] = r0 + r < rows ? (unsigned)(r * (unsigned)(ld * SZ) + c * 16) : NOWHERE;
+      }
+      kpos[0] = ((tid % 8) ^ (tid / 8 & 7)) * (16 / SZ);
+    } else {
+      base = (const unsigned char*)p + ((size_t)k0 * ld + r0) * SZ;
+      advance = (long)BK * ld * SZ;
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        const int q = tid + j * NT, k = q / PER, c = (q % PER) ^ swizzle(k);
+        kpos[j] = k;
+        off[j] = r0 + c * (16 / SZ) < rows ? (unsigned)(k * (unsigned)(ld * SZ) + c * 16) : NOWHERE;
+      }
+    }
+  }
+  // the tile of the next step; `left`: how much of k there is from its start on
+  __device__ __forceinline__ void load(unsigned lds, int wave, int left) {
+    const u32x4 res = resource(base);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+      to_lds(res, kpos[KC ? 0 : j] < left ? off[j] : NOWHERE, (unsigned)__builtin_amdgcn_readfirstlane((int)(lds + (wave * 64 + j * NT) * 16)));
+    base += advance;
+  }
+};
+
+// Fragment reads of a wave: rows [wbase + 32 i, ..), k = 16 s / SZ * 2 ..
+template <typename T, int R, bool KC, int TILES> struct Reader {
+  static constexpr int SZ = sizeof(T), RB = R * SZ;
+  unsigned at[KC ? 1 : TILES], flip;
+  __device__ __forceinline__ void init(int wbase, int lane) {
+    const int l32 = lane & 31, hi = lane >> 5;
+    if (KC) {
+      at[0] = (wbase + l32) * 128;
+      flip = ((hi ^ (lane & 7)) << 4);
+    } else if (SZ == 2) {
+      const int i = lane & 15, k = hi * 8 + i / 4;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const int byte = (wbase + t * 32 + ((lane >> 4) & 1) * 16 + (i % 4) * 4) * 2;
+        at[t] = k * RB + (byte ^ (Operand<T, R, KC, 64>::swizzle(k) << 4));
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) at[t] = hi * 4 * RB + (((wbase + t * 32 + l32) * 4) ^ (hi << 7));
+    }
+  }
+  __device__ __forceinline__ typename Frag<T>::t get(const unsigned char* tile, int t, int s) const {
+    if (KC) return *reinterpret_cast<const typename Frag<T>::t*>(tile + at[0] + t * 4096 + (flip ^ (s << 5)));
+    if constexpr (SZ == 2) {
+      typedef short tr4_t __attribute__((ext_vector_type(4)));
+      typedef tr4_t __attribute__((address_space(3))) * lds_ptr_t;
+      const unsigned char* p = tile + at[t] + s * 16 * RB;
+      const uint2 l = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p)));
+      const uint2 h = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 4 * RB)));
+      return __builtin_bit_cast(typename Frag<T>::t, make_uint4(l.x, l.y, h.x, h.y));
+    } else {
+      const unsigned char* p = tile + at[t] + s * 8 * RB;
+      return typename Frag<T>::t{*(const float*)p, *(const float*)(p + RB), *(const float*)(p + 2 * RB), *(const float*)(p + 3 * RB)};
+    }
+  }
+};
+
+enum { EXP = 1, OUT = 2 };
+
+template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, int EPI>
+__global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
+  constexpr int NT = WM * WN * 64, MT = BM / WM / 32, NTL = BN / WN / 32, BK = 128 / (int)sizeof(T), STEPS = 4;
+  typedef Operand<T, BM, AKC, NT> OpA;
+  typedef Operand<T, BN, BKC, NT> OpB;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, hi = lane >> 5;
+
+  int N = a.N, K = a.K;
+  if (a.count) {
+    int there = *a.count - a.first;
+    there = there < 0 ? 0 : there;
+    if (a.dynamic == 1) N = there < N ? there : N;
+    else K = there < K ? there : K;
+  }
+  // Workgroups go to the 8 XCDs round-robin: each XCD gets a run of neighbouring tiles, in bands of 8 along n, which share operands in its L2
+  const int tiles = a.tiles_m * a.tiles_n, total = tiles * a.splits, xcd = blockIdx.x & 7, q8 = total >> 3, r8 = total & 7;
+  int id = q8 * xcd + (xcd < r8 ? xcd : r8) + (blockIdx.x >> 3);
+  const int split = id / tiles;
+  id -= split * tiles;
+  const int band = id / (8 * a.tiles_m), in_band = id - band * 8 * a.tiles_m, wide = a.tiles_n - band * 8 < 8 ? a.tiles_n - band * 8 : 8;
+  const int tm = in_band / wide, tn = band * 8 + in_band % wide, m0 = tm * BM, n0 = tn * BN;
+  if (n0 >= N) return;
+
+  const int ksteps = (K + BK - 1) / BK, k_lo = (int)((long)ksteps * split / a.splits), k_hi = (int)((long)ksteps * (split + 1) / a.splits);
+  OpA la; OpB lb;
+  la.init(a.A, a.lda, m0, a.M, k_lo * BK, tid);
+  lb.init(a.B, a.ldb, n0, N, k_lo * BK, tid);
+  Reader<T, BM, AKC, MT> ra; Reader<T, BN, BKC, NTL> rb;
+  ra.init(wm * (BM / WM), lane);
+  rb.init(wn * (BN / WN), lane);
+  const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+  constexpr int STAGE = OpA::BYTES + OpB::BYTES;
+
+  f32x16_t acc[MT][NTL];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NTL; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  if (k_lo < k_hi) {
+    la.load(lds, wave, K - k_lo * BK);
+    lb.load(lds + OpA::BYTES, wave, K - k_lo * BK);
+  }
+  // Two stages: the loads of step t + 1 are requested when every wave is past step t - 1, whose stage they fill, and are waited for after step t
+  for (int t = k_lo; t < k_hi; ++t) {
+    step_barrier();
+    const unsigned stage = (t - k_lo) & 1;
+    if (t + 1 < k_hi) {
+      const unsigned next = lds + (stage ^ 1) * STAGE;
+      la.load(next, wave, K - (t + 1) * BK);
+      lb.load(next + OpA::BYTES, wave, K - (t + 1) * BK);
+    }
+    const unsigned char* at = smem + stage * STAGE;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      typename Frag<T>::t fa[MT], fb[NTL];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fa[i] = ra.get(at, i, s);
+#pragma unroll
+      for (int j = 0; j < NTL; ++j) fb[j] = rb.get(at + OpA::BYTES, j, s);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) acc[i][j] = Frag<T>::mma(fa[i], fb[j], acc[i][j]);
+    }
+  }
+
+  // A lane holds column n = l32 of each 32 x 32 tile, rows 8 g + 4 hi + 0..3
+  const int mw = m0 + wm * (BM / WM) + 4 * hi, nw = n0 + wn * (BN / WN) + l32;
+  if (EPI == EXP) {
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) {
+      const int n = nw + 32 * j;
+      if (m0 + BM > a.M) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) if (mw + 32 * i + 8 * (e / 4) + e % 4 >= a.M) acc[i][j][e] = -__builtin_inff();
+      }
+      const int t = n < N ? a.target[a.first + n] - mw : -1;
+      if (t >= 0 && t < 32 * MT && (t & 4) == 0 && mw + t < a.M) {   // the target is one of this lane's rows
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z = t == 32 * i + 8 * (e / 4) + e % 4 ? acc[i][j][e] : z;
+        a.zt[a.first + n] = z;
+      }
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float from = top == -__builtin_inff() ? 0.f : top;       // all of them -inf, or past the vocabulary: exp gives 0
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          acc[i][j][e] = __expf(acc[i][j][e] - from);
+          sum += acc[i][j][e];
+        }
+      sum += __shfl_xor(sum, 32);
+      if (hi == 0 && n < N) a.stat[(size_t)n * a.stats + tm * WM + wm] = make_float2(from, sum);
+      if (!a.e || n >= N) continue;
+      T* row = (T*)a.e + (size_t)n * a.lde;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int m = mw + 32 * i + 8 * g;
+          if (m < a.lde) Store<T>::store4(row + m, acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+        }
+    }
+  } else {
+    const float scale = a.scale ? *a.scale : 1.f;
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) {
+      const int n = nw + 32 * j;
+      if (n >= N) continue;
+      const size_t row = a.map ? a.map[a.first + n] : n;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int m = mw + 32 * i + 8 * g;
+          if (m >= a.M) continue;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = acc[i][j][4 * g + e] * scale;
+            if (a.prev && m + e < a.M) v[e] += a.prev[(size_t)n * a.ldp + m + e];
+          }
+          const size_t at = a.split_stride * split + row * a.ldo + m;
+          if (a.vec) {
+            if (a.out_f32) Store<float>::store4((float*)a.out + at, v[0], v[1], v[2], v[3]);
+            else Store<T>::store4((T*)a.out + at, v[0], v[1], v[2], v[3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (m + e < a.M) {
+                if (a.out_f32) ((float*)a.out)[at + e] = v[e];
+                else Store<T>::store1((T*)a.out + at + e, v[e]);
+              }
+          }
+        }
+    }
+  }
+}
+
+// ---- what lies between the products --------------------------------------------------------------
+
+__device__ __forceinline__ float wave_total(float v) {
+  v = row_sum16(v);
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// Tokens with a target, in order: idx (their places), their targets, pos (place among them, -1 without one); their count, and what the products of
+// P are multiplied by in the end, in 32 bits: 1 / count, or the largest weight (P then holds weights relative to it: equal ones are not rounded). One workgroup.
+__global__ __launch_bounds__(1024) void vocab_scan_kernel(const int* target, const float* weight, int T, int* idx, int* kept, int* pos, int* count, float* share) {
+  __shared__ int s_wave[16];
+  __shared__ float s_top[16];
+  float top = 0.f;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int before = 0;
+  for (int t0 = 0; t0 < T; t0 += 1024) {
+    const int t = t0 + tid, y = t < T ? target[t] : -1;
+    const uint64_t mask = __ballot(y >= 0);
+    if (lane == 0) s_wave[wave] = __popcll(mask);
+    __syncthreads();
+    int at = before, all = 0;
+    for (int i = 0; i < 16; ++i) { if (i < wave) at += s_wave[i]; all += s_wave[i]; }
+    at += __popcll(mask & ((1ull << lane) - 1));
+    if (t < T) {
+      pos[t] = y >= 0 ? at : -1;
+      if (y >= 0) {
+        idx[at] = t; kept[at] = y;
+        if (weight) top = fmaxf(top, fabsf(weight[t]));
+      }
+    }
+    before += all;
+    __syncthreads();
+  }
+  for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+  if (lane == 0) s_top[wave] = top;
+  __syncthreads();
+  if (tid) return;
+  for (int i = 1; i < 16; ++i) top = fmaxf(top, s_top[i]);
+  *count = before;
+  *share = !weight ? 1.f / (float)(before > 0 ? before : 1) : top > 0x1p-100f && top < 0x1p100f ? top : 1.f;
+}
+
+// A workgroup a row: row t of `from` to row pos[t] of `to` (pos null: t), widened to a whole number of 16-byte pieces with zeros. Without a place: the
+// token's results, which are zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long ld, int dim, int dim_p, bool vec, const int* pos, T* to, T* dh, long ld_dh,
+                                                           float* row_loss, float* lse) {
+  constexpr int V = Store<T>::VEC;
+  const int t = blockIdx.x, j = pos ? pos[t] : t;
+  if (j < 0) {
+    if (threadIdx.x == 0) { row_loss[t] = 0.f; if (lse) lse[t] = 0.f; }
+    if (dh) for (int c = threadIdx.x; c < dim; c += 256) dh[(size_t)t * ld_dh + c] = T{};
+    return;
+  }
+  const T* in = from + (size_t)t * ld;
+  T* out = to + (size_t)j * dim_p;
+  for (int c = threadIdx.x * V; c < dim_p; c += 256 * V) {
+    if (vec) {
+      *reinterpret_cast<uint4*>(out + c) = *reinterpret_cast<const uint4*>(in + c);
+    } else {
+      T e[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = c + i < dim ? in[c + i] : T{};
+      uint4 q;
+      __builtin_memcpy(&q, e, 16);
+      *reinterpret_cast<uint4*>(out + c) = q;
+    }
+  }
+}
+
+struct RowArgs {
+  float2* stat; int stats, stat_cols;
+  const float* zt; const int* target; const int* idx; const int* count; const float* weight; const float* share;
+  int first, rows, V;
+  float* row_loss; float* lse;
+  void* p; long ld; int chunk;       // gradients: exp(z - m), turned into P; columns of a workgroup
+};
+
+// The log-sum of a token from its maxima and sums, its loss, and its row of P: a workgroup takes a chunk of the row (blockIdx.x), each of
+// them joins the maxima and sums for itself.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_row_kernel(RowArgs a) {
+  constexpr int V = Store<T>::VEC;
+  __shared__ float red[2][4];
+  const int r = blockIdx.y, tid = threadIdx.x;
+  if (a.count && a.first + r >= *a.count) return;
+  const float2* st = a.stat + (size_t)r * a.stats;
+  float top = -__builtin_inff();
+  for (int i = tid; i < a.stats; i += 256) {
+    const float2 v = st[i];
+    top = fmaxf(top, v.y != 0.f ? v.x : -__builtin_inff());      // (a NaN sum counts)
+  }
+  top = fmaxf(top, __shfl_xor(top, 1)); top = fmaxf(top, __shfl_xor(top, 2)); top = fmaxf(top, __shfl_xor(top, 4));
+  top = fmaxf(top, __shfl_xor(top, 8)); top = fmaxf(top, __shfl_xor(top, 16)); top = fmaxf(top, __shfl_xor(top, 32));
+  if ((tid & 63) == 0) red[0][tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  const int at = a.first + r, token = a.idx ? a.idx[at] : at, y = a.target[at];
+  const bool has = y >= 0 && y < a.V;
+  const float zt = has ? a.zt[at] : __builtin_nanf("");             // a target past the vocabulary: its loss is NaN, nothing is read for it
+  const float from = top == -__builtin_inff() ? 0.f : top;
+  float sum = 0.f;
+  for (int i = tid; i < a.stats; i += 256) {
+    const float2 v = st[i];
+    if (v.y != 0.f) sum += v.y * __expf(v.x - from);
+  }
+  sum = wave_total(sum);
+  if ((tid & 63) == 0) red[1][tid >> 6] = sum;
+  __syncthreads();
+  sum = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+  const float lse = from + logf(sum);
+  if (blockIdx.x == 0 && tid == 0) {
+    if (a.row_loss) a.row_loss[token] = y < 0 ? 0.f : lse - zt;
+    if (a.lse) a.lse[token] = y < 0 ? 0.f : lse;
+  }
+  if (!a.p) return;
+  const float share = a.weight ? a.weight[token] / *a.share : 1.f;
+  T* row = (T*)a.p + (size_t)r * a.ld;
+  const int lo = blockIdx.x * a.chunk, hi = lo + a.chunk < a.ld ? lo + a.chunk : (int)a.ld;
+  for (int c = lo + tid * V; c < hi; c += 256 * V) {
+    float v[V];
+    Store<T>::load_vec(row + c, v);
+    const float scale = c < a.V ? __expf(st[c / a.stat_cols].x - lse) * share : 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      v[e] = c + e < a.V ? v[e] * scale : 0.f;
+      if (c + e == y) v[e] = (__expf(zt - from) / sum - 1.f) * share;
+    }
+    Store<T>::store_vec(row + c, v);
+  }
+}
+
+// dh from the parts of the vocabulary, in their order
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_join_kernel(const float* part, int splits, size_t stride, int dim, const int* count, int first, int rows,
+                                                         const float* scale, const int* map, T* dh, long ld) {
+  const int r = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (c >= dim || (count && first + r >= *count)) return;
+  const int wide = (dim + 3) & ~3;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) {
+    const float4 q = *reinterpret_cast<const float4*>(part + s * stride + (size_t)r * wide + c);
+    v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+  }
+  T* out = dh + (size_t)(map ? map[first + r] : first + r) * ld + c;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) if (c + e < dim) Store<T>::store1(out + e, v[e] * *scale);
+}
+
+// The loss: the tokens' losses, weighted, in a fixed order and in 64 bits. One workgroup.
+__global__ __launch_bounds__(1024) void vocab_total_kernel(const int* target, const float* row_loss, const float* weight, int T, float* loss) {
+  __shared__ double red[16];
+  __shared__ int n_red[16];
+  const int tid = threadIdx.x;
+  double t = 0.0;
+  int n = 0;
+  for (int i = tid; i < T; i += 1024) {
+    if (target[i] < 0) continue;
+    t += weight ? (double)row_loss[i] * weight[i] : (double)row_loss[i];
+    ++n;
+  }
+  for (int k = 1; k < 64; k <<= 1) { t += __shfl_xor(t, k); n += __shfl_xor(n, k); }
+  if ((tid & 63) == 0) { red[tid >> 6] = t; n_red[tid >> 6] = n; }
+  __syncthreads();
+  if (tid) return;
+  t = 0.0; n = 0;
+  for (int i = 0; i < 16; ++i) { t += red[i]; n += n_red[i]; }
+  *loss = (float)(weight ? t : t / (n > 0 ? n : 1));
+}
+
+// ---- launches ------------------------------------------------------------------------------------
+
+enum { LARGE = 0, MEDIUM = 1, FEW = 2 };
+struct Tile { int bm, bn, wm, wn; };
+constexpr Tile TILES[] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {128, 32, 4, 1}};
+
+template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, int EPI>
+hipError_t product_run(const ProductArgs& a, hipStream_t s) {
+  constexpr int LDS = 2 * (BM + BN) * 128;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&product_kernel<T, BM, BN, WM, WN, AKC, BKC, EPI>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  if (attr != hipSuccess) return attr;
+  DDG_LAUNCH((product_kernel<T, BM, BN, WM, WN, AKC, BKC, EPI>), dim3(a.tiles_m * a.tiles_n * a.splits), dim3(WM * WN * 64), LDS, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, bool AKC, bool BKC, int EPI>
+hipError_t product_any(ProductArgs a, int cfg, hipStream_t s) {
+  a.tiles_m = (a.M + TILES[cfg].bm - 1) / TILES[cfg].bm;
+  a.tiles_n = (a.N + TILES[cfg].bn - 1) / TILES[cfg].bn;
+  if (a.tiles_n == 0) return hipSuccess;
+  if constexpr (sizeof(T) == 2) if (cfg == LARGE) return product_run<T, 256, 256, 2, 4, AKC, BKC, EPI>(a, s);
+  if constexpr (BKC) if (cfg == FEW) return product_run<T, 128, 32, 4, 1, AKC, BKC, EPI>(a, s);
+  return product_run<T, 128, 128, 2, 2, AKC, BKC, EPI>(a, s);
+}
+
+size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
+int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
+
+constexpr size_t PANEL_BYTES = ((size_t)1 << 30) + ((size_t)1 << 24);    // of a panel's P: 4096 tokens of a vocabulary of 131072 in bf16, a quarter of what 8192 logits in fp32 take
+
+}  // namespace
+
+void vocab_plan(VocabPlan* p) {
+  const size_t size = dtype_size(p->dtype);
+  const int vec = 16 / (int)size, few = 32;
+  p->dim_p = (int)up(p->dim, vec);
+  p->ld_p = (long)up(p->vocab, 64) + 64;           // (rows an odd number of 128 bytes apart where the vocabulary is a power of two)
+  p->pack_h = p->grads || p->pack_h || p->tokens > 64;
+  const size_t row = p->grads ? p->ld_p * size : (size_t)p->vocab / 4 + 64;
+  long most = (long)(PANEL_BYTES / row / 256 * 256);
+  if (most < 256) most = 256;
+  p->panels = p->tokens > most ? ceil_div(p->tokens, most) : 1;
+  p->panel = p->panels > 1 ? (int)up(ceil_div(p->tokens, p->panels), 256) : p->tokens;
+  if (p->panels > 1) p->panels = ceil_div(p->tokens, p->panel);
+  const bool b16 = size == 2;
+  auto tiles = [&](int cfg, long m, long n) { return (long)ceil_div(m, TILES[cfg].bm) * ceil_div(n, TILES[cfg].bn); };
+  p->cfg_z = p->panel <= few ? FEW : b16 && p->panel > 128 && tiles(LARGE, p->vocab, p->panel) >= 128 ? LARGE : MEDIUM;
+  p->cfg_dh = p->panel <= few ? FEW : b16 && p->panel > 128 && p->dim > 128 ? LARGE : MEDIUM;
+  p->cfg_dw = b16 && p->panel > 128 && tiles(LARGE, p->dim, p->vocab) >= 128 ? LARGE : MEDIUM;
+  p->stat_cols = TILES[p->cfg_z].bm / TILES[p->cfg_z].wm;
+  p->stats = ceil_div(p->vocab, TILES[p->cfg_z].bm) * TILES[p->cfg_z].wm;
+  const long t = tiles(p->cfg_dh, p->dim, p->panel), want = p->cfg_dh == LARGE ? 256 : 768, steps = ceil_div((long)p->vocab * size, 128);
+  long splits = t > 0 ? (want + t / 2) / t : 1;
+  if (splits > steps / 4) splits = steps / 4;
+  p->splits = splits < 1 ? 1 : (int)splits;
+  p->acc = p->grads && p->panels > 1 && !p->dw_f32 && b16;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes, 256); return o; };
+  const size_t T = p->tokens;
+  p->o_scalar = take(256);
+  p->o_row = take(T * 16);                          // idx, kept targets, places, losses
+  p->o_zt = take(T * 4);
+  p->o_stat = take((size_t)p->panel * p->stats * 8);
+  p->o_p = p->grads ? take((size_t)p->panel * p->ld_p * size) : 0;
+  p->o_part = p->grads && p->splits > 1 ? take((size_t)p->splits * p->panel * up(p->dim, 4) * 4) : 0;
+  p->o_acc = p->acc ? take((size_t)p->vocab * up(p->dim, 4) * 4) : 0;
+  p->o_h = p->pack_h ? take(T * p->dim_p * size) : 0;
+  p->o_w = p->pack_w ? take((size_t)p->vocab * p->dim_p * size) : 0;
+  p->bytes = at;
+}
+
+namespace {
+
+#define TRY(expr)                       \
+  do {                                  \
+    const hipError_t e_ = (expr);       \
+    if (e_ != hipSuccess) return e_;    \
+  } while (0)
+
+template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& a, hipStream_t s) {
+  const size_t size = sizeof(T);
+  int* count = (int*)(a.ws + p.o_scalar);
+  float* share = (float*)(a.ws + p.o_scalar) + 1;
+  int* idx = (int*)(a.ws + p.o_row), *kept = idx + p.tokens, *pos = kept + p.tokens;
+  float* row_loss = a.row_loss ? a.row_loss : (float*)(pos + p.tokens);
+  float* zt = (float*)(a.ws + p.o_zt);
+  float2* stat = (float2*)(a.ws + p.o_stat);
+  const T* h = (const T*)a.h; const T* w = (const T*)a.w;
+  long ld_h = a.ld_h, ld_w = a.ld_w;
+  if (p.pack_h) {
+    DDG_LAUNCH(vocab_scan_kernel, dim3(1), dim3(1024), 0, s, a.target, a.weight, p.tokens, idx, kept, pos, count, share);
+    TRY(hipGetLastError());
+    if (p.tokens) {
+      const bool vec = p.dim == p.dim_p && (uintptr_t)a.h % 16 == 0 && ld_h * size % 16 == 0;
+      DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.tokens), dim3(256), 0, s, h, ld_h, p.dim, p.dim_p, vec, (const int*)pos, (T*)(a.ws + p.o_h), (T*)a.dh, a.ld_dh,
+                 row_loss, a.lse);
+      TRY(hipGetLastError());
+    }
+    h = (const T*)(a.ws + p.o_h); ld_h = p.dim_p;
+  }
+  if (p.pack_w) {
+    DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.vocab), dim3(256), 0, s, w, ld_w, p.dim, p.dim_p, false, (const int*)nullptr, (T*)(a.ws + p.o_w), (T*)nullptr, 0L,
+               (float*)nullptr, (float*)nullptr);
+    TRY(hipGetLastError());
+    w = (const T*)(a.ws + p.o_w); ld_w = p.dim_p;
+  }
+  const int* bound = p.pack_h ? count : nullptr;
+  for (int panel = 0; panel < p.panels; ++panel) {
+    const int first = panel * p.panel, rows = p.tokens - first < p.panel ? p.tokens - first : p.panel;
+    ProductArgs z{};
+    z.A = w; z.lda = ld_w; z.B = h + (size_t)first * ld_h; z.ldb = ld_h; z.M = p.vocab; z.N = rows; z.K = p.dim_p; z.splits = 1;
+    z.count = bound; z.first = first; z.dynamic = 1;
+    z.e = p.grads ? a.ws + p.o_p : nullptr; z.lde = p.ld_p; z.stat = stat; z.stats = p.stats; z.target = p.pack_h ? kept : a.target; z.zt = zt;
+    TRY((product_any<T, true, true, EXP>(z, p.cfg_z, s)));
+    if (rows) {
+      RowArgs r{};
+      r.stat = stat; r.stats = p.stats; r.stat_cols = p.stat_cols; r.zt = zt; r.target = z.target; r.idx = p.pack_h ? idx : nullptr; r.count = bound;
+      r.weight = a.weight; r.share = share; r.first = first; r.rows = rows; r.V = p.vocab; r.row_loss = row_loss; r.lse = a.lse;
+      int chunks = 1;
+      if (p.grads) {
+        r.p = a.ws + p.o_p; r.ld = p.ld_p;
+        // enough workgroups to fill the chip, none with less than two trips
+        const int unit = 2 * 256 * Store<T>::VEC, most = ceil_div(p.ld_p, unit);
+        chunks = ceil_div(2048, rows);
+        if (chunks > most) chunks = most;
+        r.chunk = (int)up(ceil_div(p.ld_p, chunks), Store<T>::VEC * 256);
+        chunks = ceil_div(p.ld_p, r.chunk);
+      }
+      for (int y = 0; y < rows; y += 65535) {       // (a grid's second dimension)
+        RowArgs q = r;
+        const int n = rows - y < 65535 ? rows - y : 65535;
+        q.first += y; q.stat += (size_t)y * q.stats; q.rows = n;
+        if (q.p) q.p = (T*)q.p + (size_t)y * q.ld;
+        DDG_LAUNCH(vocab_row_kernel<T>, dim3(chunks, n), dim3(256), 0, s, q);
+        TRY(hipGetLastError());
+      }
+    }
+    if (!p.grads) continue;
+    const bool vec_dim = p.dim % 4 == 0;
+    if (a.dh && rows) {
+      ProductArgs g{};
+      g.A = w; g.lda = ld_w; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = rows; g.K = p.vocab; g.splits = p.splits;
+      g.count = bound; g.first = first; g.dynamic = 1;
+      if (p.splits > 1) {
+        g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)rows * g.ldo; g.vec = vec_dim;
+      } else {
+        g.out = a.dh; g.ldo = a.ld_dh; g.map = idx; g.scale = share; g.out_f32 = size == 4;
+        g.vec = vec_dim && (uintptr_t)a.dh % (4 * size) == 0 && a.ld_dh % 4 == 0;
+      }
+      TRY((product_any<T, false, true, OUT>(g, p.cfg_dh, s)));
+      if (p.splits > 1) {
+        for (int y = 0; y < rows; y += 65535) {
+          const int n = rows - y < 65535 ? rows - y : 65535;
+          DDG_LAUNCH(vocab_join_kernel<T>, dim3(ceil_div(p.dim, 1024), n), dim3(256), 0, s, (const float*)g.out + (size_t)y * g.ldo, p.splits, g.split_stride,
+                     p.dim, bound, first + y, n, (const float*)share, (const int*)idx, (T*)a.dh, a.ld_dh);
+          TRY(hipGetLastError());
+        }
+      }
+    }
+    if (a.dw) {
+      ProductArgs g{};
+      g.A = h + (size_t)first * ld_h; g.lda = ld_h; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = p.vocab; g.K = rows; g.splits = 1;
+      g.count = bound; g.first = first; g.dynamic = 2; g.scale = share;
+      const bool f32 = size == 4 || p.dw_f32, last = panel + 1 == p.panels;
+      float* sum = p.acc ? (float*)(a.ws + p.o_acc) : (float*)a.dw;
+      const long ld_sum = p.acc ? (long)up(p.dim, 4) : a.ld_dw;
+      if (panel) { g.prev = sum; g.ldp = ld_sum; }
+      g.out_f32 = f32 || !last;
+      g.out = !last ? (void*)sum : a.dw; g.ldo = !last ? ld_sum : a.ld_dw;
+      g.vec = vec_dim && (uintptr_t)g.out % (g.out_f32 ? 16 : 8) == 0 && g.ldo % 4 == 0;
+      TRY((product_any<T, false, false, OUT>(g, p.cfg_dw, s)));
+    }
+  }
+  if (a.loss) {
+    DDG_LAUNCH(vocab_total_kernel, dim3(1), dim3(1024), 0, s, a.target, (const float*)row_loss, a.weight, p.tokens, a.loss);
+    TRY(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t vocab_launch(const VocabPlan& p, const VocabArgs& a, hipStream_t s) {
+  return p.dtype == BF16 ? vocab_run<bf16_t>(p, a, s) : vocab_run<float>(p, a, s);
+}
+
+}  // namespace ddg

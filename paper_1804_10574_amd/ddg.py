@@ -39,6 +39,23 @@ class ModuleDesc(C.Structure):
                 ("stale_jacobian", C.c_int)]
 
 
+class DropoutDesc(C.Structure):
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int), ("dtype", C.c_int), ("p", C.c_float), ("seed", C.c_uint64),
+                ("ld_x", C.c_long), ("ld_y", C.c_long), ("stream", C.c_void_p), ("dry_run", C.c_int)]
+
+
+class JoinDesc(C.Structure):
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int), ("dtype", C.c_int), ("eps", C.c_float), ("p", C.c_float),
+                ("seed", C.c_uint64), ("ld_y", C.c_long), ("ld_residual", C.c_long), ("ld_x", C.c_long),
+                ("ld_out", C.c_long), ("group", C.c_int), ("stream", C.c_void_p), ("dry_run", C.c_int)]
+
+
+class VocabDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int), ("dim", C.c_int), ("vocab", C.c_int), ("dtype", C.c_int), ("ld_h", C.c_long),
+                ("ld_w", C.c_long), ("ld_dh", C.c_long), ("ld_dw", C.c_long), ("dw_f32", C.c_int),
+                ("stream", C.c_void_p), ("dry_run", C.c_int)]
+
+
 _lib = None
 
 
@@ -108,6 +125,13 @@ def load_library():
         "ddg_profile_read": (st, [vp, C.c_int, C.POINTER(C.c_long), C.POINTER(C.c_double),
                                   C.POINTER(C.c_double), C.POINTER(C.c_double)]),
         "ddg_profile_reset": (st, [vp]),
+        "ddg_dropout": (st, [C.POINTER(DropoutDesc), C.c_uint64, vp, vp]),
+        "ddg_join_norm": (st, [C.POINTER(JoinDesc), C.c_uint64] + [vp] * 6),
+        "ddg_join_norm_q8": (st, [C.POINTER(JoinDesc), C.c_uint64] + [vp] * 7),
+        "ddg_join_norm_workspace": (C.c_size_t, [C.POINTER(JoinDesc)]),
+        "ddg_join_norm_backward": (st, [C.POINTER(JoinDesc), C.c_uint64] + [vp] * 9 + [C.c_size_t]),
+        "ddg_vocab_loss_workspace": (C.c_size_t, [C.POINTER(VocabDesc), C.c_int]),
+        "ddg_vocab_loss": (st, [C.POINTER(VocabDesc)] + [vp] * 10 + [C.c_size_t]),
         "ddg_last_error": (C.c_char_p, []),
         "ddg_version": (C.c_char_p, []),
     }
@@ -131,6 +155,8 @@ EXPORTS = ["ddg_module_create", "ddg_module_destroy", "ddg_param_count", "ddg_ou
            "ddg_ring_slots", "ddg_ring_slot_bytes", "ddg_get_ring_slot", "ddg_set_ring_slot", "ddg_set_time", "ddg_get_time",
            "ddg_pipeline_time", "ddg_pipeline_set_time", "ddg_pipeline_mail_bytes", "ddg_pipeline_get_mail",
            "ddg_pipeline_set_mail",
+           "ddg_dropout", "ddg_join_norm", "ddg_join_norm_q8", "ddg_join_norm_workspace", "ddg_join_norm_backward",
+           "ddg_vocab_loss_workspace", "ddg_vocab_loss",
            "ddg_last_error", "ddg_version"]
 
 
@@ -412,3 +438,61 @@ class Pipeline:
         it = C.c_long()
         _check(self._lib.ddg_pipeline_get_delta(self._h, k, _ptr(out), C.byref(it)))
         return (out, it.value) if it.value >= 0 else (None, -1)
+
+
+# ---- operators of token models: a descriptor each, tensors and workspace are the caller's --------
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size() if hasattr(t, "data_ptr") else t.nbytes
+
+
+class Dropout:
+    """ddg_dropout on [rows][cols]: the same call on the error gradient is its backward pass."""
+
+    def __init__(self, rows, cols, dtype, p, seed=0, ld_x=0, ld_y=0, stream=None, dry_run=False):
+        self._lib = load_library()
+        self.desc = DropoutDesc(rows, cols, dtype, p, seed, ld_x, ld_y, stream, 1 if dry_run else 0)
+
+    def __call__(self, x, y, step=0):
+        _check(self._lib.ddg_dropout(self.desc, step, _ptr(x), _ptr(y)))
+
+
+class JoinNorm:
+    """Join of a residual branch with its norm: ddg_join_norm, ddg_join_norm_q8, ddg_join_norm_backward."""
+
+    def __init__(self, rows, cols, dtype, eps=1e-6, p=0.0, seed=0, ld_y=0, ld_residual=0, ld_x=0, ld_out=0, group=0,
+                 stream=None, dry_run=False):
+        self._lib = load_library()
+        self.desc = JoinDesc(rows, cols, dtype, eps, p, seed, ld_y, ld_residual, ld_x, ld_out, group, stream,
+                             1 if dry_run else 0)
+
+    def workspace_bytes(self) -> int:
+        """Bytes that `backward` needs for d_gain."""
+        return int(self._lib.ddg_join_norm_workspace(self.desc))
+
+    def forward(self, y, residual, gain, out, x_out=None, rstd=None, step=0):
+        _check(self._lib.ddg_join_norm(self.desc, step, _ptr(y), _ptr(residual), _ptr(gain), _ptr(x_out), _ptr(out), _ptr(rstd)))
+
+    def forward_q8(self, y, residual, gain, q, scale, x_out=None, rstd=None, step=0):
+        _check(self._lib.ddg_join_norm_q8(self.desc, step, _ptr(y), _ptr(residual), _ptr(gain), _ptr(x_out), _ptr(q), _ptr(scale),
+                                          _ptr(rstd)))
+
+    def backward(self, x, rstd, gain, d_out, d_x=None, d_residual=None, d_y=None, d_gain=None, workspace=None, step=0):
+        _check(self._lib.ddg_join_norm_backward(self.desc, step, _ptr(x), _ptr(rstd), _ptr(gain), _ptr(d_out), _ptr(d_x),
+                                                _ptr(d_residual), _ptr(d_y), _ptr(d_gain), _ptr(workspace), _bytes(workspace)))
+
+
+class VocabLoss:
+    """ddg_vocab_loss: softmax cross entropy over a vocabulary and its gradients, without the logits."""
+
+    def __init__(self, tokens, dim, vocab, dtype, ld_h=0, ld_w=0, ld_dh=0, ld_dw=0, dw_f32=False, stream=None, dry_run=False):
+        self._lib = load_library()
+        self.desc = VocabDesc(tokens, dim, vocab, dtype, ld_h, ld_w, ld_dh, ld_dw, 1 if dw_f32 else 0, stream,
+                              1 if dry_run else 0)
+
+    def workspace_bytes(self, gradients=True) -> int:
+        return int(self._lib.ddg_vocab_loss_workspace(self.desc, 1 if gradients else 0))
+
+    def __call__(self, h, w, targets, weights=None, loss=None, row_loss=None, lse=None, dh=None, dw=None, workspace=None):
+        _check(self._lib.ddg_vocab_loss(self.desc, _ptr(h), _ptr(w), _ptr(targets), _ptr(weights), _ptr(loss), _ptr(row_loss),
+                                        _ptr(lse), _ptr(dh), _ptr(dw), _ptr(workspace), _bytes(workspace)))
