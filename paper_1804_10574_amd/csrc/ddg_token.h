@@ -41,7 +41,7 @@ struct VocabPlan {
   long ld_p;                 // elements between the rows of the panel's probabilities
   int cfg_z, cfg_dh, cfg_dw; // tiles of the three products
   int stat_cols, stats;      // columns that share a maximum and sum, and their number
-  int splits;                // parts of the vocabulary that dh is summed over
+  int splits, splits_dw;     // parts of the vocabulary that dh is summed over, of the tokens that dw is
   bool acc;                  // dw is summed over panels in a buffer of the workspace
   size_t o_scalar, o_row, o_zt, o_stat, o_p, o_part, o_acc, o_h, o_w, bytes;
 };

@@ -9,6 +9,8 @@
 #include "ddg_device.h"
 #include "ddg_token.h"
 
+#include <type_traits>
+
 namespace ddg {
 namespace {
 
@@ -28,7 +30,7 @@ struct ProductArgs {
   void* e; long lde; float2* stat; int stats; const int* target; float* zt;
   // epilogue 2: out[map[n]][m] = scale * sum + prev
   void* out; long ldo; int out_f32; const float* prev; long ldp; const float* scale; const int* map; size_t split_stride;
-  int vec;                   // rows of `out` are 4-element pieces
+  int vec;                   // rows of `out` are pieces of a store: 16 bytes (OUT), 4 elements (SUM)
 };
 
 // 16 bytes a lane from memory straight to LDS, at `lds` + 16 * lane; lanes at NOWHERE write zeros. Nothing waits here: the load has no output register,
@@ -36,10 +38,11 @@ struct ProductArgs {
 __device__ __forceinline__ void to_lds(u32x4 res, unsigned voff, unsigned lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(res) : "memory");
 }
-// Every load of this wave has arrived and every LDS read has been answered, in all waves
-__device__ __forceinline__ void step_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// All but the last PENDING loads of this wave have arrived and every LDS read has been answered, in all waves
+template <int PENDING> __device__ __forceinline__ void step_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
 }
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ u32x4 resource(const void* p) {
   const uint64_t a = (uint64_t)(uintptr_t)p;
   return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)a), (unsigned)__builtin_amdgcn_readfirstlane((int)((unsigned)(a >> 32) & 0xffffu)),
@@ -146,11 +149,21 @@ template <typename T, int R, bool KC, int TILES> struct Reader {
   }
 };
 
-enum { EXP = 1, OUT = 2 };
+// Epilogues: EXP (product 1), OUT (results in the operands' type), SUM (through 32 bits: added to earlier sums, or left in fp32)
+enum { EXP = 1, OUT = 2, SUM = 3 };
 
-template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, int EPI>
+template <typename T, int BM, int BN, int WM, int WN, int STAGES, int EPI> struct ProductShape {
+  typedef std::conditional_t<EPI == SUM, float, T> Staged;
+  static constexpr int NT = WM * WN * 64, STAGE = (BM + BN) * 128;
+  // the tile on its way out: 32 rows of each wave column at a time, rows 16 bytes apart in the banks
+  static constexpr int PITCH = BM * (int)sizeof(Staged) + 16, LEAVING = WN * 32 * PITCH;
+  static constexpr int LDS = STAGES * STAGE > LEAVING ? STAGES * STAGE : LEAVING;
+};
+
+template <typename T, int BM, int BN, int WM, int WN, int STAGES, bool AKC, bool BKC, int EPI>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
-  constexpr int NT = WM * WN * 64, MT = BM / WM / 32, NTL = BN / WN / 32, BK = 128 / (int)sizeof(T), STEPS = 4;
+  typedef ProductShape<T, BM, BN, WM, WN, STAGES, EPI> Shape;
+  constexpr int NT = Shape::NT, MT = BM / WM / 32, NTL = BN / WN / 32, BK = 128 / (int)sizeof(T), STEPS = 4, STAGE = Shape::STAGE;
   typedef Operand<T, BM, AKC, NT> OpA;
   typedef Operand<T, BN, BKC, NT> OpB;
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -181,7 +194,6 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
   ra.init(wm * (BM / WM), lane);
   rb.init(wn * (BN / WN), lane);
   const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-  constexpr int STAGE = OpA::BYTES + OpB::BYTES;
 
   f32x16_t acc[MT][NTL];
 #pragma unroll
@@ -191,20 +203,24 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  if (k_lo < k_hi) {
-    la.load(lds, wave, K - k_lo * BK);
-    lb.load(lds + OpA::BYTES, wave, K - k_lo * BK);
-  }
-  // Two stages: the loads of step t + 1 are requested when every wave is past step t - 1, whose stage they fill, and are waited for after step t
+  auto load = [&](int t, unsigned stage) __attribute__((always_inline)) {
+    la.load(lds + stage * STAGE, wave, K - t * BK);
+    lb.load(lds + stage * STAGE + OpA::BYTES, wave, K - t * BK);
+  };
+#pragma unroll
+  for (int t = 0; t < STAGES - 1; ++t) if (k_lo + t < k_hi) load(k_lo + t, t);
+  // The loads of step t + STAGES - 1 are requested when every wave is past step t - 1, whose stage they fill; step t waits for its own only
+  unsigned stage = 0, next = STAGES - 1;
   for (int t = k_lo; t < k_hi; ++t) {
-    step_barrier();
-    const unsigned stage = (t - k_lo) & 1;
-    if (t + 1 < k_hi) {
-      const unsigned next = lds + (stage ^ 1) * STAGE;
-      la.load(next, wave, K - (t + 1) * BK);
-      lb.load(next + OpA::BYTES, wave, K - (t + 1) * BK);
+    if (t + STAGES - 1 < k_hi) {
+      step_barrier<(STAGES - 2) * (OpA::LOADS + OpB::LOADS)>();
+      load(t + STAGES - 1, next);
+    } else {
+      step_barrier<0>();
     }
     const unsigned char* at = smem + stage * STAGE;
+    stage = stage == STAGES - 1 ? 0 : stage + 1;
+    next = next == STAGES - 1 ? 0 : next + 1;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       typename Frag<T>::t fa[MT], fb[NTL];
@@ -219,11 +235,12 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
     }
   }
 
-  // A lane holds column n = l32 of each 32 x 32 tile, rows 8 g + 4 hi + 0..3
+  // A lane holds column n = l32 of each 32 x 32 tile, rows 8 g + 4 hi + 0..3. Rows of the result leave through LDS, so that a wave's stores are whole lines.
   const int mw = m0 + wm * (BM / WM) + 4 * hi, nw = n0 + wn * (BN / WN) + l32;
-  if (EPI == EXP) {
+  const float scale = EPI != EXP && a.scale ? *a.scale : 1.f;
 #pragma unroll
-    for (int j = 0; j < NTL; ++j) {
+  for (int j = 0; j < NTL; ++j) {
+    if (EPI == EXP) {
       const int n = nw + 32 * j;
       if (m0 + BM > a.M) {
 #pragma unroll
@@ -257,48 +274,54 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
         }
       sum += __shfl_xor(sum, 32);
       if (hi == 0 && n < N) a.stat[(size_t)n * a.stats + tm * WM + wm] = make_float2(from, sum);
-      if (!a.e || n >= N) continue;
-      T* row = (T*)a.e + (size_t)n * a.lde;
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int m = mw + 32 * i + 8 * g;
-          if (m < a.lde) Store<T>::store4(row + m, acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
-        }
+      if (!a.e) continue;
     }
-  } else {
-    const float scale = a.scale ? *a.scale : 1.f;
+    typedef typename Shape::Staged S;
+    constexpr int V = EPI == SUM ? 4 : 16 / (int)sizeof(T), PIECES = BM / V, ROWS = WN * 32;
+    lds_barrier();
 #pragma unroll
-    for (int j = 0; j < NTL; ++j) {
-      const int n = nw + 32 * j;
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        Store<S>::store4(reinterpret_cast<S*>(smem + (wn * 32 + l32) * Shape::PITCH) + wm * (BM / WM) + 32 * i + 8 * g + 4 * hi, acc[i][j][4 * g] * scale,
+                         acc[i][j][4 * g + 1] * scale, acc[i][j][4 * g + 2] * scale, acc[i][j][4 * g + 3] * scale);
+    lds_barrier();
+#pragma unroll
+    for (int q = 0; q < ROWS * PIECES / NT; ++q) {
+      const int at = tid + q * NT, r = at / PIECES, c = at % PIECES;
+      const int n = n0 + (r / 32) * (BN / WN) + 32 * j + r % 32, m = m0 + c * V;
       if (n >= N) continue;
-      const size_t row = a.map ? a.map[a.first + n] : n;
+      const S* from = reinterpret_cast<const S*>(smem + r * Shape::PITCH) + c * V;
+      if (EPI == EXP) {
+        if (m < a.lde) *reinterpret_cast<uint4*>((T*)a.e + (size_t)n * a.lde + m) = *reinterpret_cast<const uint4*>(from);
+        continue;
+      }
+      if (m >= a.M) continue;
+      const size_t to = a.split_stride * split + (size_t)(a.map ? a.map[a.first + n] : n) * a.ldo + m;
+      if (EPI == OUT) {
+        if (a.vec) {
+          *reinterpret_cast<uint4*>((T*)a.out + to) = *reinterpret_cast<const uint4*>(from);
+        } else {
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int m = mw + 32 * i + 8 * g;
-          if (m >= a.M) continue;
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = acc[i][j][4 * g + e] * scale;
-            if (a.prev && m + e < a.M) v[e] += a.prev[(size_t)n * a.ldp + m + e];
-          }
-          const size_t at = a.split_stride * split + row * a.ldo + m;
-          if (a.vec) {
-            if (a.out_f32) Store<float>::store4((float*)a.out + at, v[0], v[1], v[2], v[3]);
-            else Store<T>::store4((T*)a.out + at, v[0], v[1], v[2], v[3]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (m + e < a.M) {
-                if (a.out_f32) ((float*)a.out)[at + e] = v[e];
-                else Store<T>::store1((T*)a.out + at + e, v[e]);
-              }
-          }
+          for (int e = 0; e < V; ++e) if (m + e < a.M) ((T*)a.out)[to + e] = reinterpret_cast<const T*>(from)[e];
         }
+      } else {
+        float v[4];
+        Store<float>::load4(reinterpret_cast<const float*>(from), v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (a.prev && m + e < a.M) v[e] += a.prev[(size_t)n * a.ldp + m + e];
+        if (a.vec) {
+          if (a.out_f32) Store<float>::store4((float*)a.out + to, v[0], v[1], v[2], v[3]);
+          else Store<T>::store4((T*)a.out + to, v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m + e < a.M) {
+              if (a.out_f32) ((float*)a.out)[to + e] = v[e];
+              else Store<T>::store1((T*)a.out + to + e, v[e]);
+            }
+        }
+      }
     }
   }
 }
@@ -436,10 +459,10 @@ __global__ __launch_bounds__(256) void vocab_row_kernel(RowArgs a) {
   }
 }
 
-// dh from the parts of the vocabulary, in their order
+// dh from the parts of the vocabulary, or dw from those of the tokens, in their order
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_join_kernel(const float* part, int splits, size_t stride, int dim, const int* count, int first, int rows,
-                                                         const float* scale, const int* map, T* dh, long ld) {
+                                                         const float* scale, const int* map, T* to, long ld) {
   const int r = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= dim || (count && first + r >= *count)) return;
   const int wide = (dim + 3) & ~3;
@@ -448,7 +471,8 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(const float* part, int 
     const float4 q = *reinterpret_cast<const float4*>(part + s * stride + (size_t)r * wide + c);
     v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
   }
-  T* out = dh + (size_t)(map ? map[first + r] : first + r) * ld + c;
+  T* out = to + (size_t)(map ? map[first + r] : first + r) * ld + c;
+
 #pragma unroll
   for (int e = 0; e < 4; ++e) if (c + e < dim) Store<T>::store1(out + e, v[e] * *scale);
 }
@@ -476,28 +500,42 @@ __global__ __launch_bounds__(1024) void vocab_total_kernel(const int* target, co
 
 // ---- launches ------------------------------------------------------------------------------------
 
-enum { LARGE = 0, MEDIUM = 1, FEW = 2 };
-struct Tile { int bm, bn, wm, wn; };
-constexpr Tile TILES[] = {{256, 256, 2, 4}, {128, 128, 2, 2}, {128, 32, 4, 1}};
+// Tiles of the products: rows along m (vocabulary or width) and n, waves along both, stages of LDS
+enum { LARGE, MEDIUM, SMALL, HALF, FEW, TILE_KINDS };
+struct Tile { int bm, bn, wm, wn, stages; };
+constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 2}, {128, 128, 2, 2, 2}, {64, 64, 2, 2, 3}, {128, 64, 4, 1, 3}, {128, 32, 4, 1, 4}};
 
-template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, int EPI>
-hipError_t product_run(const ProductArgs& a, hipStream_t s) {
-  constexpr int LDS = 2 * (BM + BN) * 128;
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&product_kernel<T, BM, BN, WM, WN, AKC, BKC, EPI>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+template <typename T, int KIND, bool AKC, bool BKC, int EPI>
+hipError_t product_run(ProductArgs a, hipStream_t s) {
+  constexpr Tile t = TILES[KIND];
+  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.stages, EPI>::LDS;
+  const auto kernel = &product_kernel<T, t.bm, t.bn, t.wm, t.wn, t.stages, AKC, BKC, EPI>;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return attr;
-  DDG_LAUNCH((product_kernel<T, BM, BN, WM, WN, AKC, BKC, EPI>), dim3(a.tiles_m * a.tiles_n * a.splits), dim3(WM * WN * 64), LDS, s, a);
+  a.tiles_m = (a.M + t.bm - 1) / t.bm;
+  a.tiles_n = (a.N + t.bn - 1) / t.bn;
+  if (a.tiles_n == 0) return hipSuccess;
+  DDG_LAUNCH(kernel, dim3(a.tiles_m * a.tiles_n * a.splits), dim3(t.wm * t.wn * 64), LDS, s, a);
   return hipGetLastError();
 }
 
 template <typename T, bool AKC, bool BKC, int EPI>
-hipError_t product_any(ProductArgs a, int cfg, hipStream_t s) {
-  a.tiles_m = (a.M + TILES[cfg].bm - 1) / TILES[cfg].bm;
-  a.tiles_n = (a.N + TILES[cfg].bn - 1) / TILES[cfg].bn;
-  if (a.tiles_n == 0) return hipSuccess;
-  if constexpr (sizeof(T) == 2) if (cfg == LARGE) return product_run<T, 256, 256, 2, 4, AKC, BKC, EPI>(a, s);
-  if constexpr (BKC) if (cfg == FEW) return product_run<T, 128, 32, 4, 1, AKC, BKC, EPI>(a, s);
-  return product_run<T, 128, 128, 2, 2, AKC, BKC, EPI>(a, s);
+hipError_t product_any(const ProductArgs& a, int kind, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) if (kind == LARGE) return product_run<T, LARGE, AKC, BKC, EPI>(a, s);
+  if constexpr (BKC) {
+    if (kind == FEW) return product_run<T, FEW, AKC, BKC, EPI>(a, s);
+    if (kind == HALF) return product_run<T, HALF, AKC, BKC, EPI>(a, s);
+  }
+  if (kind == SMALL) return product_run<T, SMALL, AKC, BKC, EPI>(a, s);
+  return product_run<T, MEDIUM, AKC, BKC, EPI>(a, s);
+}
+// results in the operands' type, or in fp32, or added to earlier ones
+template <typename T, bool AKC, bool BKC> hipError_t product_out(ProductArgs a, size_t dim, int kind, hipStream_t s) {
+  const bool sum = sizeof(T) == 4 || a.out_f32 || a.prev;
+  const size_t piece = sum ? 4 : 8, bytes = piece * (a.out_f32 || sizeof(T) == 4 ? 4 : 2);
+  a.vec = dim % piece == 0 && (uintptr_t)a.out % bytes == 0 && a.ldo % piece == 0 && a.split_stride % piece == 0;
+  a.out_f32 = a.out_f32 || sizeof(T) == 4;
+  return sum ? product_any<T, AKC, BKC, SUM>(a, kind, s) : product_any<T, AKC, BKC, OUT>(a, kind, s);
 }
 
 size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
@@ -509,7 +547,7 @@ constexpr size_t PANEL_BYTES = ((size_t)1 << 30) + ((size_t)1 << 24);    // of a
 
 void vocab_plan(VocabPlan* p) {
   const size_t size = dtype_size(p->dtype);
-  const int vec = 16 / (int)size, few = 32;
+  const int vec = 16 / (int)size;
   p->dim_p = (int)up(p->dim, vec);
   p->ld_p = (long)up(p->vocab, 64) + 64;           // (rows an odd number of 128 bytes apart where the vocabulary is a power of two)
   p->pack_h = p->grads || p->pack_h || p->tokens > 64;
@@ -520,16 +558,27 @@ void vocab_plan(VocabPlan* p) {
   p->panel = p->panels > 1 ? (int)up(ceil_div(p->tokens, p->panels), 256) : p->tokens;
   if (p->panels > 1) p->panels = ceil_div(p->tokens, p->panel);
   const bool b16 = size == 2;
-  auto tiles = [&](int cfg, long m, long n) { return (long)ceil_div(m, TILES[cfg].bm) * ceil_div(n, TILES[cfg].bn); };
-  p->cfg_z = p->panel <= few ? FEW : b16 && p->panel > 128 && tiles(LARGE, p->vocab, p->panel) >= 128 ? LARGE : MEDIUM;
-  p->cfg_dh = p->panel <= few ? FEW : b16 && p->panel > 128 && p->dim > 128 ? LARGE : MEDIUM;
-  p->cfg_dw = b16 && p->panel > 128 && tiles(LARGE, p->dim, p->vocab) >= 128 ? LARGE : MEDIUM;
+  // n at most 64: tiles of that many columns; else the largest tile with one for half the compute units or more, and for the sums of dh and dw
+  // (results of any size, long sums) with parts of the sum to fill the chip
+  auto choose = [&](long m, long n, long k, bool parts, bool few_ok, int* kind, int* splits) {
+    const long steps = ceil_div(k * (long)size, 128);
+    auto tiles = [&](int c) { return (long)ceil_div(m, TILES[c].bm) * ceil_div(n, TILES[c].bn); };
+    if (few_ok && n <= 64) *kind = n <= 32 ? FEW : HALF;
+    else if (b16 && n > 128 && m > 128 && tiles(LARGE) * (parts ? steps / 8 : 1) >= 128) *kind = LARGE;
+    else if (tiles(MEDIUM) * (parts ? steps / 8 : 1) >= 128) *kind = MEDIUM;
+    else *kind = SMALL;
+    const long want = *kind == LARGE ? 256 : *kind == MEDIUM ? 512 : 768, t = tiles(*kind) < 1 ? 1 : tiles(*kind);
+    long q = parts ? (want + t / 2) / t : 1;
+    if (q > steps / 4) q = steps / 4;
+    *splits = q < 1 ? 1 : (int)q;
+  };
+  int one;
+  choose(p->vocab, p->panel, p->dim_p, false, true, &p->cfg_z, &one);
+  choose(p->dim, p->panel, p->vocab, true, true, &p->cfg_dh, &p->splits);
+  choose(p->dim, p->vocab, p->panel, true, false, &p->cfg_dw, &p->splits_dw);
+  if (p->panels > 1) p->splits_dw = 1;
   p->stat_cols = TILES[p->cfg_z].bm / TILES[p->cfg_z].wm;
   p->stats = ceil_div(p->vocab, TILES[p->cfg_z].bm) * TILES[p->cfg_z].wm;
-  const long t = tiles(p->cfg_dh, p->dim, p->panel), want = p->cfg_dh == LARGE ? 256 : 768, steps = ceil_div((long)p->vocab * size, 128);
-  long splits = t > 0 ? (want + t / 2) / t : 1;
-  if (splits > steps / 4) splits = steps / 4;
-  p->splits = splits < 1 ? 1 : (int)splits;
   p->acc = p->grads && p->panels > 1 && !p->dw_f32 && b16;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes, 256); return o; };
@@ -539,7 +588,8 @@ void vocab_plan(VocabPlan* p) {
   p->o_zt = take(T * 4);
   p->o_stat = take((size_t)p->panel * p->stats * 8);
   p->o_p = p->grads ? take((size_t)p->panel * p->ld_p * size) : 0;
-  p->o_part = p->grads && p->splits > 1 ? take((size_t)p->splits * p->panel * up(p->dim, 4) * 4) : 0;
+  const size_t part = p->splits > 1 ? (size_t)p->splits * p->panel : 0, part_dw = p->splits_dw > 1 ? (size_t)p->splits_dw * p->vocab : 0;
+  p->o_part = p->grads ? take((part > part_dw ? part : part_dw) * up(p->dim, 4) * 4) : 0;
   p->o_acc = p->acc ? take((size_t)p->vocab * up(p->dim, 4) * 4) : 0;
   p->o_h = p->pack_h ? take(T * p->dim_p * size) : 0;
   p->o_w = p->pack_w ? take((size_t)p->vocab * p->dim_p * size) : 0;
@@ -613,39 +663,47 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       }
     }
     if (!p.grads) continue;
-    const bool vec_dim = p.dim % 4 == 0;
+    // the parts of a sum, joined into rows `map` of `out`
+    auto join = [&](const ProductArgs& g, int n, int splits, const int* limit, const int* map, int at, auto* out, long ld) -> hipError_t {
+      for (int y = 0; y < n; y += 65535) {
+        const int some = n - y < 65535 ? n - y : 65535;
+        DDG_LAUNCH((vocab_join_kernel<std::remove_pointer_t<decltype(out)>>), dim3(ceil_div(p.dim, 1024), some), dim3(256), 0, s,
+                   (const float*)g.out + (size_t)y * g.ldo, splits, g.split_stride, p.dim, limit, at + y, some, (const float*)share, map, out, ld);
+        TRY(hipGetLastError());
+      }
+      return hipSuccess;
+    };
     if (a.dh && rows) {
       ProductArgs g{};
       g.A = w; g.lda = ld_w; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = rows; g.K = p.vocab; g.splits = p.splits;
       g.count = bound; g.first = first; g.dynamic = 1;
       if (p.splits > 1) {
-        g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)rows * g.ldo; g.vec = vec_dim;
+        g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)rows * g.ldo;
       } else {
-        g.out = a.dh; g.ldo = a.ld_dh; g.map = idx; g.scale = share; g.out_f32 = size == 4;
-        g.vec = vec_dim && (uintptr_t)a.dh % (4 * size) == 0 && a.ld_dh % 4 == 0;
+        g.out = a.dh; g.ldo = a.ld_dh; g.map = idx; g.scale = share;
       }
-      TRY((product_any<T, false, true, OUT>(g, p.cfg_dh, s)));
-      if (p.splits > 1) {
-        for (int y = 0; y < rows; y += 65535) {
-          const int n = rows - y < 65535 ? rows - y : 65535;
-          DDG_LAUNCH(vocab_join_kernel<T>, dim3(ceil_div(p.dim, 1024), n), dim3(256), 0, s, (const float*)g.out + (size_t)y * g.ldo, p.splits, g.split_stride,
-                     p.dim, bound, first + y, n, (const float*)share, (const int*)idx, (T*)a.dh, a.ld_dh);
-          TRY(hipGetLastError());
-        }
-      }
+      TRY((product_out<T, false, true>(g, p.dim, p.cfg_dh, s)));
+      if (p.splits > 1) TRY(join(g, rows, p.splits, bound, idx, first, (T*)a.dh, a.ld_dh));
     }
     if (a.dw) {
       ProductArgs g{};
-      g.A = h + (size_t)first * ld_h; g.lda = ld_h; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = p.vocab; g.K = rows; g.splits = 1;
-      g.count = bound; g.first = first; g.dynamic = 2; g.scale = share;
+      g.A = h + (size_t)first * ld_h; g.lda = ld_h; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = p.vocab; g.K = rows; g.splits = p.splits_dw;
+      g.count = bound; g.first = first; g.dynamic = 2;
+      if (p.splits_dw > 1) {
+        g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)p.vocab * g.ldo;
+        TRY((product_out<T, false, false>(g, p.dim, p.cfg_dw, s)));
+        if (p.dw_f32) TRY(join(g, p.vocab, p.splits_dw, nullptr, nullptr, 0, (float*)a.dw, a.ld_dw));
+        else TRY(join(g, p.vocab, p.splits_dw, nullptr, nullptr, 0, (T*)a.dw, a.ld_dw));
+        continue;
+      }
       const bool f32 = size == 4 || p.dw_f32, last = panel + 1 == p.panels;
       float* sum = p.acc ? (float*)(a.ws + p.o_acc) : (float*)a.dw;
       const long ld_sum = p.acc ? (long)up(p.dim, 4) : a.ld_dw;
       if (panel) { g.prev = sum; g.ldp = ld_sum; }
+      g.scale = share;
       g.out_f32 = f32 || !last;
       g.out = !last ? (void*)sum : a.dw; g.ldo = !last ? ld_sum : a.ld_dw;
-      g.vec = vec_dim && (uintptr_t)g.out % (g.out_f32 ? 16 : 8) == 0 && g.ldo % 4 == 0;
-      TRY((product_any<T, false, false, OUT>(g, p.cfg_dw, s)));
+      TRY((product_out<T, false, false>(g, p.dim, p.cfg_dw, s)));
     }
   }
   if (a.loss) {
