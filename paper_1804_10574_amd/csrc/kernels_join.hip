@@ -408,11 +408,11 @@ template <typename T, bool VEC> hipError_t backward_any(const JoinArgs& a, hipSt
 
 }  // namespace
 
-// 2048 waves, and a workgroup a compute unit at least: fewer leave the memory idle (8192 x 2048 in bf16: 35.8 us with 256 workgroups of 4 waves, 32.4 with 512,
+// Two workgroups of up to 4 waves a compute unit, or one of more: fewer leave the memory idle (8192 x 2048 in bf16: 35.8 us with 256 workgroups of 4 waves, 32.4 with 512,
 // 37.2 with 1024), and more mean more rows to add up afterwards
 int join_groups(int rows, int cols) {
   const int upr = (cols + 7) / 8, per = upr <= 64 ? 4 : 1;
-  const int most = upr <= 64 ? 512 : upr <= 128 ? 1024 : upr <= 256 ? 512 : 256, want = (rows + per - 1) / per;
+  const int most = upr <= 256 ? 512 : 256, want = (rows + per - 1) / per;
   return want < 1 ? 1 : want < most ? want : most;
 }
 

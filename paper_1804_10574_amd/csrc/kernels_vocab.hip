@@ -10,6 +10,7 @@
 #include "ddg_token.h"
 
 #include <type_traits>
+#include <stdlib.h>
 
 namespace ddg {
 namespace {
@@ -27,7 +28,7 @@ struct ProductArgs {
   int first, dynamic;        // first token of the panel
   int tiles_m, tiles_n, splits;
   // epilogue 1: exp(z - m), maxima and sums, the target's logit
-  void* e; long lde; float2* stat; int stats; const int* target; float* zt;
+  void* e; long lde; float2* stat; int stats; const int* target; float* zt;   // stat: [N][stats], one of each wave's columns
   // epilogue 2: out[map[n]][m] = scale * sum + prev
   void* out; long ldo; int out_f32; const float* prev; long ldp; const float* scale; const int* map; size_t split_stride;
   int vec;                   // rows of `out` are pieces of a store: 16 bytes (OUT), 4 elements (SUM)
@@ -64,18 +65,20 @@ template <> struct Frag<float> {
   }
 };
 
-// One operand's tile of a step in LDS: R rows of the tile by 128 bytes of k.
-//   KC: [R][128 bytes], 16-byte piece c of row r at place c ^ (r & 7): the 32 rows that a fragment read takes at one k spread over all banks.
+// One operand's tile of a step in LDS: R rows of the tile by KB bytes of k, 128 or 64.
+//   KC: [R][KB bytes], 16-byte piece c of row r at place c ^ f(r), f = r >> 1 & 7 (KB 64: r >> 2 & 3): any 16 neighbouring rows have a fragment's pieces in
+//   different banks (two or four rows to the 256 bytes of all banks).
 //   else: [BK][R], whose fragments are read transposed; 64-byte pieces (bf16: 32 columns) of row k at place piece ^ (k & 3), so that the four
 //   rows of a transposing read lie in different banks (R = 64: two rows to 256 bytes, place ^ (k >> 1 & 1)); fp32: 128-byte pieces, place ^ (k >> 2 & 1).
-template <typename T, int R, bool KC, int NT> struct Operand {
-  static constexpr int SZ = sizeof(T), BK = 128 / SZ, BYTES = R * 128, LOADS = R * 8 / NT, RB = R * SZ, PER = RB / 16;
-  static_assert(LOADS >= 1 && R * 8 % NT == 0, "every thread loads");
+template <typename T, int R, int KB, bool KC, int NT> struct Operand {
+  static constexpr int SZ = sizeof(T), BK = KB / SZ, BYTES = R * KB, ROW = KB / 16, LOADS = R * ROW / NT, RB = R * SZ, PER = RB / 16;
+  static_assert(LOADS >= 1 && R * ROW % NT == 0, "every thread loads");
   unsigned off[LOADS];       // bytes from the step's base
   int kpos[KC ? 1 : LOADS];  // k of the loads (KC: of all)
   const unsigned char* base;
   long advance;
 
+  static __device__ __forceinline__ int place(int r) { return KB == 128 ? r >> 1 & 7 : r >> 2 & 3; }
   static __device__ __forceinline__ int swizzle(int k) {    // in 16-byte pieces
     if (SZ == 4) return ((k >> 2) & 1) << 3;
     return RB >= 256 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
@@ -83,14 +86,15 @@ template <typename T, int R, bool KC, int NT> struct Operand {
   // rows [r0, r0 + R) of `rows`, from k0 on
   __device__ __forceinline__ void init(const void* p, long ld, int r0, int rows, int k0, int tid) {
     if (KC) {
+      static_assert(!KC || NT / ROW % 16 == 0, "one place for all loads of a thread");
       base = (const unsigned char*)p + ((size_t)r0 * ld + k0) * SZ;
-      advance = 128;
+      advance = KB;
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) {
-        const int r = tid / 8 + j * (NT / 8), c = (tid % 8) ^ (r & 7);
+        const int r = tid / ROW + j * (NT / ROW), c = (tid % ROW) ^ place(r);
         off[j] = r0 + r < rows ? (unsigned)(r * (unsigned)(ld * SZ) + c * 16) : NOWHERE;
       }
-      kpos[0] = ((tid % 8) ^ (tid / 8 & 7)) * (16 / SZ);
+      kpos[0] = ((tid % ROW) ^ place(tid / ROW)) * (16 / SZ);
     } else {
       base = (const unsigned char*)p + ((size_t)k0 * ld + r0) * SZ;
       advance = (long)BK * ld * SZ;
@@ -102,31 +106,29 @@ template <typename T, int R, bool KC, int NT> struct Operand {
       }
     }
   }
-  // the tile of the next step; `left`: how much of k there is from its start on
-  __device__ __forceinline__ void load(unsigned lds, int wave, int left) {
-    const u32x4 res = resource(base);
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j)
-      to_lds(res, kpos[KC ? 0 : j] < left ? off[j] : NOWHERE, (unsigned)__builtin_amdgcn_readfirstlane((int)(lds + (wave * 64 + j * NT) * 16)));
-    base += advance;
+  // load j of a step's tile, through its resource; `left`: how much of k there is from the step's start on
+  __device__ __forceinline__ void load(const u32x4 res, unsigned lds, int wave, int left, int j) const {
+    to_lds(res, kpos[KC ? 0 : j] < left ? off[j] : NOWHERE, (unsigned)__builtin_amdgcn_readfirstlane((int)(lds + (wave * 64 + j * NT) * 16)));
   }
+  __device__ __forceinline__ void step() { base += advance; }
 };
 
 // Fragment reads of a wave: rows [wbase + 32 i, ..), k = 16 s / SZ * 2 ..
-template <typename T, int R, bool KC, int TILES> struct Reader {
+template <typename T, int R, int KB, bool KC, int TILES> struct Reader {
   static constexpr int SZ = sizeof(T), RB = R * SZ;
+  typedef Operand<T, R, KB, KC, 64> Op;
   unsigned at[KC ? 1 : TILES], flip;
   __device__ __forceinline__ void init(int wbase, int lane) {
     const int l32 = lane & 31, hi = lane >> 5;
     if (KC) {
-      at[0] = (wbase + l32) * 128;
-      flip = ((hi ^ (lane & 7)) << 4);
+      at[0] = (wbase + l32) * KB;
+      flip = (hi ^ Op::place(l32)) << 4;
     } else if (SZ == 2) {
       const int i = lane & 15, k = hi * 8 + i / 4;
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
         const int byte = (wbase + t * 32 + ((lane >> 4) & 1) * 16 + (i % 4) * 4) * 2;
-        at[t] = k * RB + (byte ^ (Operand<T, R, KC, 64>::swizzle(k) << 4));
+        at[t] = k * RB + (byte ^ (Op::swizzle(k) << 4));
       }
     } else {
 #pragma unroll
@@ -134,7 +136,7 @@ template <typename T, int R, bool KC, int TILES> struct Reader {
     }
   }
   __device__ __forceinline__ typename Frag<T>::t get(const unsigned char* tile, int t, int s) const {
-    if (KC) return *reinterpret_cast<const typename Frag<T>::t*>(tile + at[0] + t * 4096 + (flip ^ (s << 5)));
+    if (KC) return *reinterpret_cast<const typename Frag<T>::t*>(tile + at[0] + t * 32 * KB + (flip ^ (s << 5)));
     if constexpr (SZ == 2) {
       typedef short tr4_t __attribute__((ext_vector_type(4)));
       typedef tr4_t __attribute__((address_space(3))) * lds_ptr_t;
@@ -152,20 +154,21 @@ template <typename T, int R, bool KC, int TILES> struct Reader {
 // Epilogues: EXP (product 1), OUT (results in the operands' type), SUM (through 32 bits: added to earlier sums, or left in fp32)
 enum { EXP = 1, OUT = 2, SUM = 3 };
 
-template <typename T, int BM, int BN, int WM, int WN, int STAGES, int EPI> struct ProductShape {
+template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, int EPI> struct ProductShape {
   typedef std::conditional_t<EPI == SUM, float, T> Staged;
-  static constexpr int NT = WM * WN * 64, STAGE = (BM + BN) * 128;
+  static constexpr int NT = WM * WN * 64, STAGE = (BM + BN) * KB;
   // the tile on its way out: 32 rows of each wave column at a time, rows 16 bytes apart in the banks
   static constexpr int PITCH = BM * (int)sizeof(Staged) + 16, LEAVING = WN * 32 * PITCH;
   static constexpr int LDS = STAGES * STAGE > LEAVING ? STAGES * STAGE : LEAVING;
 };
 
-template <typename T, int BM, int BN, int WM, int WN, int STAGES, bool AKC, bool BKC, int EPI>
-__global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
-  typedef ProductShape<T, BM, BN, WM, WN, STAGES, EPI> Shape;
-  constexpr int NT = Shape::NT, MT = BM / WM / 32, NTL = BN / WN / 32, BK = 128 / (int)sizeof(T), STEPS = 4, STAGE = Shape::STAGE;
-  typedef Operand<T, BM, AKC, NT> OpA;
-  typedef Operand<T, BN, BKC, NT> OpB;
+template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool AKC, bool BKC, int EPI>
+__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
+  typedef ProductShape<T, BM, BN, WM, WN, KB, STAGES, EPI> Shape;
+  constexpr int NT = Shape::NT, MT = BM / WM / 32, NTL = BN / WN / 32, BK = KB / (int)sizeof(T), STEPS = KB / 32, STAGE = Shape::STAGE;
+  constexpr bool INTERLEAVED = MT * NTL >= 8;
+  typedef Operand<T, BM, KB, AKC, NT> OpA;
+  typedef Operand<T, BN, KB, BKC, NT> OpB;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, hi = lane >> 5;
@@ -188,13 +191,24 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
 
   const int ksteps = (K + BK - 1) / BK, k_lo = (int)((long)ksteps * split / a.splits), k_hi = (int)((long)ksteps * (split + 1) / a.splits);
   OpA la; OpB lb;
-  la.init(a.A, a.lda, m0, a.M, k_lo * BK, tid);
-  lb.init(a.B, a.ldb, n0, N, k_lo * BK, tid);
-  Reader<T, BM, AKC, MT> ra; Reader<T, BN, BKC, NTL> rb;
+  // Where every workgroup has rows of A of its own, each begins at another k: all of them at the same one would read a column of A at a time, whose pieces
+  // lie a row apart, in few of the memory's channels
+  const int turn = EPI == EXP && MT * NTL < 8 && a.tiles_n <= 2 && k_hi > k_lo ? tm % (k_hi - k_lo) : 0;
+  la.init(a.A, a.lda, m0, a.M, (k_lo + turn) * BK, tid);
+  lb.init(a.B, a.ldb, n0, N, (k_lo + turn) * BK, tid);
+  Reader<T, BM, KB, AKC, MT> ra; Reader<T, BN, KB, BKC, NTL> rb;
   ra.init(wm * (BM / WM), lane);
   rb.init(wn * (BN / WN), lane);
   const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
 
+  int aim[NTL];              // EXP: the targets of this lane's tokens
+  if (EPI == EXP) {
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) {
+      const int n = n0 + wn * (BN / WN) + 32 * j + l32;
+      aim[j] = n < N ? a.target[a.first + n] : -1;
+    }
+  }
   f32x16_t acc[MT][NTL];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -203,35 +217,99 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
+  constexpr int PER_STEP = OpA::LOADS + OpB::LOADS, AHEAD = STAGES - 1;
   auto load = [&](int t, unsigned stage) __attribute__((always_inline)) {
-    la.load(lds + stage * STAGE, wave, K - t * BK);
-    lb.load(lds + stage * STAGE + OpA::BYTES, wave, K - t * BK);
+    const u32x4 res_a = resource(la.base), res_b = resource(lb.base);
+#pragma unroll
+    for (int j = 0; j < OpA::LOADS; ++j) la.load(res_a, lds + stage * STAGE, wave, K - t * BK, j);
+#pragma unroll
+    for (int j = 0; j < OpB::LOADS; ++j) lb.load(res_b, lds + stage * STAGE + OpA::BYTES, wave, K - t * BK, j);
+    la.step(); lb.step();
   };
-#pragma unroll
-  for (int t = 0; t < STAGES - 1; ++t) if (k_lo + t < k_hi) load(k_lo + t, t);
-  // The loads of step t + STAGES - 1 are requested when every wave is past step t - 1, whose stage they fill; step t waits for its own only
-  unsigned stage = 0, next = STAGES - 1;
-  for (int t = k_lo; t < k_hi; ++t) {
-    if (t + STAGES - 1 < k_hi) {
-      step_barrier<(STAGES - 2) * (OpA::LOADS + OpB::LOADS)>();
-      load(t + STAGES - 1, next);
-    } else {
-      step_barrier<0>();
+  int at_k = k_lo + turn;    // the next step that is requested: the first one is `turn`, after the last comes k_lo
+  auto request = [&](unsigned stage) __attribute__((always_inline)) {
+    load(at_k, stage);
+    if (++at_k == k_hi) {
+      at_k = k_lo;
+      la.base -= (k_hi - k_lo) * la.advance; lb.base -= (k_hi - k_lo) * lb.advance;
     }
-    const unsigned char* at = smem + stage * STAGE;
-    stage = stage == STAGES - 1 ? 0 : stage + 1;
-    next = next == STAGES - 1 ? 0 : next + 1;
+  };
+  if constexpr (INTERLEAVED) {
+    // The matrix instructions of a step in a row, and one LDS read of the next k's fragments or one load between each two: a wave never has a burst of
+    // others to issue first (product 2 of 4096 tokens of 131072 entries and width 4096: 3.06 ms, 3.29 with the waves in two groups that take turns at LDS and the matrix
+    // pipes, 3.53 with the reads of each k before its instructions). Before a step's last k every wave has read all of its stage; there the next
+    // step's loads are waited for. Step t requests step t + AHEAD into the stage of step t - 1. Loads past the end of k are made, and write zeros: the counts are constant.
+    static_assert(STAGES >= 3 && PER_STEP % STEPS == 0, "");
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      typename Frag<T>::t fa[MT], fb[NTL];
+    for (int t = 0; t < AHEAD; ++t) load(k_lo + t, t);
+    typename Frag<T>::t fa[2][MT], fb[2][NTL];
+    step_barrier<(AHEAD - 1) * PER_STEP>();
 #pragma unroll
-      for (int i = 0; i < MT; ++i) fa[i] = ra.get(at, i, s);
+    for (int i = 0; i < MT; ++i) fa[0][i] = ra.get(smem, i, 0);
 #pragma unroll
-      for (int j = 0; j < NTL; ++j) fb[j] = rb.get(at + OpA::BYTES, j, s);
+    for (int j = 0; j < NTL; ++j) fb[0][j] = rb.get(smem + OpA::BYTES, j, 0);
+    unsigned stage = 0, before = STAGES - 1;
+    for (int t = k_lo; t < k_hi; ++t) {
+      const unsigned next = stage == STAGES - 1 ? 0 : stage + 1, fill = lds + before * STAGE;
+      const u32x4 res_a = resource(la.base), res_b = resource(lb.base);
+      const int left = K - (t + AHEAD) * BK;
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int s = 0; s < STEPS; ++s) {
+        const bool last = s == STEPS - 1;
+        if (last) step_barrier<(AHEAD - 2) * PER_STEP + PER_STEP * (STEPS - 1) / STEPS>();
+        const unsigned char* at = smem + (last ? next : stage) * STAGE;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < NTL; ++j) acc[i][j] = Frag<T>::mma(fa[i], fb[j], acc[i][j]);
+        for (int q = 0; q < MT * NTL; ++q) {
+          constexpr int EVERY = MT * NTL / (MT + NTL);
+          acc[q % MT][q / MT] = Frag<T>::mma(fa[s & 1][q % MT], fb[s & 1][q / MT], acc[q % MT][q / MT]);
+          if (q % EVERY == 0 && q / EVERY < MT + NTL) {
+            const int f = q / EVERY;
+            if (f < MT) fa[(s + 1) & 1][f] = ra.get(at, f, last ? 0 : s + 1);
+            else fb[(s + 1) & 1][f - MT] = rb.get(at + OpA::BYTES, f - MT, last ? 0 : s + 1);
+          }
+#pragma unroll
+          for (int d = 0; d < PER_STEP; ++d)
+            if (d * MT * NTL * STEPS / PER_STEP == s * MT * NTL + q) {
+              if (d < OpA::LOADS) la.load(res_a, fill, wave, left, d);
+              else lb.load(res_b, fill + OpA::BYTES, wave, left, d - OpA::LOADS);
+            }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      la.step(); lb.step();
+      before = stage;
+      stage = next;
+    }
+    step_barrier<0>();
+  } else {
+    // Few instructions a step: several workgroups of a compute unit fill each other's gaps. Step t waits for its own loads only, and requests those of step
+    // t + AHEAD when every wave is past step t - 1, whose stage they fill.
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) if (k_lo + t < k_hi) request(t);
+    unsigned stage = 0, next = AHEAD;
+    for (int t = k_lo; t < k_hi; ++t) {
+      if (t + AHEAD < k_hi) {
+        step_barrier<(AHEAD - 1) * PER_STEP>();
+        request(next);
+      } else {
+        step_barrier<0>();
+      }
+      const unsigned char* at = smem + stage * STAGE;
+      stage = stage == STAGES - 1 ? 0 : stage + 1;
+      next = next == STAGES - 1 ? 0 : next + 1;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        typename Frag<T>::t fa[MT], fb[NTL];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[i] = ra.get(at, i, s);
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) fb[j] = rb.get(at + OpA::BYTES, j, s);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NTL; ++j) acc[i][j] = Frag<T>::mma(fa[i], fb[j], acc[i][j]);
+      }
     }
   }
 
@@ -248,7 +326,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) if (mw + 32 * i + 8 * (e / 4) + e % 4 >= a.M) acc[i][j][e] = -__builtin_inff();
       }
-      const int t = n < N ? a.target[a.first + n] - mw : -1;
+      const int t = aim[j] < 0 ? -1 : aim[j] - mw;
       if (t >= 0 && t < 32 * MT && (t & 4) == 0 && mw + t < a.M) {   // the target is one of this lane's rows
         float z = 0.f;
 #pragma unroll
@@ -278,6 +356,18 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
     }
     typedef typename Shape::Staged S;
     constexpr int V = EPI == SUM ? 4 : 16 / (int)sizeof(T), PIECES = BM / V, ROWS = WN * 32;
+    float4 prev[EPI == SUM ? ROWS * PIECES / NT : 1];
+    if (EPI == SUM && a.prev) {          // requested before the tile goes through LDS
+#pragma unroll
+      for (int q = 0; q < ROWS * PIECES / NT; ++q) {
+        const int r = (tid + q * NT) / PIECES, n = n0 + (r / 32) * (BN / WN) + 32 * j + r % 32, m = m0 + (tid + q * NT) % PIECES * V;
+        prev[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (n >= N || m >= a.M) continue;
+        const float* from = a.prev + (size_t)n * a.ldp + m;
+        if (a.vec) prev[q] = *reinterpret_cast<const float4*>(from);
+        else prev[q] = make_float4(from[0], m + 1 < a.M ? from[1] : 0.f, m + 2 < a.M ? from[2] : 0.f, m + 3 < a.M ? from[3] : 0.f);
+      }
+    }
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -308,8 +398,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductArgs a) {
       } else {
         float v[4];
         Store<float>::load4(reinterpret_cast<const float*>(from), v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) if (a.prev && m + e < a.M) v[e] += a.prev[(size_t)n * a.ldp + m + e];
+        if (a.prev) { v[0] += prev[q].x; v[1] += prev[q].y; v[2] += prev[q].z; v[3] += prev[q].w; }
         if (a.vec) {
           if (a.out_f32) Store<float>::store4((float*)a.out + to, v[0], v[1], v[2], v[3]);
           else Store<T>::store4((T*)a.out + to, v[0], v[1], v[2], v[3]);
@@ -398,7 +487,7 @@ __global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long l
 }
 
 struct RowArgs {
-  float2* stat; int stats, stat_cols;
+  const float2* stat; int stats, stat_cols;   // [rows][stats]: maxima and sums of columns
   const float* zt; const int* target; const int* idx; const int* count; const float* weight; const float* share;
   int first, rows, V;
   float* row_loss; float* lse;
@@ -500,16 +589,16 @@ __global__ __launch_bounds__(1024) void vocab_total_kernel(const int* target, co
 
 // ---- launches ------------------------------------------------------------------------------------
 
-// Tiles of the products: rows along m (vocabulary or width) and n, waves along both, stages of LDS
+// Tiles of the products: rows along m (vocabulary or width) and n, waves along both, bytes of k in a stage, stages of LDS
 enum { LARGE, MEDIUM, SMALL, HALF, FEW, TILE_KINDS };
-struct Tile { int bm, bn, wm, wn, stages; };
-constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 2}, {128, 128, 2, 2, 2}, {64, 64, 2, 2, 3}, {128, 64, 4, 1, 3}, {128, 32, 4, 1, 4}};
+struct Tile { int bm, bn, wm, wn, kb, stages; };
+constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 64, 4}, {128, 128, 2, 2, 128, 2}, {64, 64, 2, 2, 128, 3}, {128, 64, 4, 1, 128, 3}, {128, 32, 4, 1, 128, 4}};
 
 template <typename T, int KIND, bool AKC, bool BKC, int EPI>
 hipError_t product_run(ProductArgs a, hipStream_t s) {
   constexpr Tile t = TILES[KIND];
-  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.stages, EPI>::LDS;
-  const auto kernel = &product_kernel<T, t.bm, t.bn, t.wm, t.wn, t.stages, AKC, BKC, EPI>;
+  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, EPI>::LDS;
+  const auto kernel = &product_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, AKC, BKC, EPI>;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return attr;
   a.tiles_m = (a.M + t.bm - 1) / t.bm;
@@ -533,7 +622,8 @@ hipError_t product_any(const ProductArgs& a, int kind, hipStream_t s) {
 template <typename T, bool AKC, bool BKC> hipError_t product_out(ProductArgs a, size_t dim, int kind, hipStream_t s) {
   const bool sum = sizeof(T) == 4 || a.out_f32 || a.prev;
   const size_t piece = sum ? 4 : 8, bytes = piece * (a.out_f32 || sizeof(T) == 4 ? 4 : 2);
-  a.vec = dim % piece == 0 && (uintptr_t)a.out % bytes == 0 && a.ldo % piece == 0 && a.split_stride % piece == 0;
+  a.vec = dim % piece == 0 && (uintptr_t)a.out % bytes == 0 && a.ldo % piece == 0 && a.split_stride % piece == 0 &&
+          (!a.prev || ((uintptr_t)a.prev % 16 == 0 && a.ldp % 4 == 0));
   a.out_f32 = a.out_f32 || sizeof(T) == 4;
   return sum ? product_any<T, AKC, BKC, SUM>(a, kind, s) : product_any<T, AKC, BKC, OUT>(a, kind, s);
 }
@@ -558,24 +648,38 @@ void vocab_plan(VocabPlan* p) {
   p->panel = p->panels > 1 ? (int)up(ceil_div(p->tokens, p->panels), 256) : p->tokens;
   if (p->panels > 1) p->panels = ceil_div(p->tokens, p->panel);
   const bool b16 = size == 2;
-  // n at most 64: tiles of that many columns; else the largest tile with one for half the compute units or more, and for the sums of dh and dw
-  // (results of any size, long sums) with parts of the sum to fill the chip
+  // The tiles, and for the sums of dh and dw (results of any size, long sums) the parts, that take the least time by what the kinds were measured at: us a
+  // step of 128 bytes of k with one workgroup on a compute unit, with as many as fit, how many do, and us for the way in and out.
+  struct Rate { float alone, full; int fit; float ends; };
+  static const Rate rates[2][TILE_KINDS] = {{{0.f, 0.f, 1, 0.f}, {2.0f, 4.1f, 2, 4.f}, {0.66f, 1.65f, 3, 3.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}},
+                                            {{1.0f, 1.45f, 1, 8.f}, {0.68f, 1.1f, 2, 4.f}, {0.28f, 0.7f, 3, 3.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}}};
   auto choose = [&](long m, long n, long k, bool parts, bool few_ok, int* kind, int* splits) {
     const long steps = ceil_div(k * (long)size, 128);
-    auto tiles = [&](int c) { return (long)ceil_div(m, TILES[c].bm) * ceil_div(n, TILES[c].bn); };
-    if (few_ok && n <= 64) *kind = n <= 32 ? FEW : HALF;
-    else if (b16 && n > 128 && m > 128 && tiles(LARGE) * (parts ? steps / 8 : 1) >= 128) *kind = LARGE;
-    else if (tiles(MEDIUM) * (parts ? steps / 8 : 1) >= 128) *kind = MEDIUM;
-    else *kind = SMALL;
-    const long want = *kind == LARGE ? 256 : *kind == MEDIUM ? 512 : 768, t = tiles(*kind) < 1 ? 1 : tiles(*kind);
-    long q = parts ? (want + t / 2) / t : 1;
-    if (q > steps / 4) q = steps / 4;
-    *splits = q < 1 ? 1 : (int)q;
+    float best = -1.f;
+    *kind = MEDIUM; *splits = 1;
+    for (int c = b16 ? LARGE : MEDIUM; c < TILE_KINDS; ++c) {
+      if (!few_ok && c > SMALL) break;
+      const Rate r = rates[b16][c];
+      const long tiles = (long)ceil_div(m, TILES[c].bm) * ceil_div(n, TILES[c].bn);
+      for (int q = 1; q <= (parts ? 64 : 1) && (q == 1 || q * 2 <= steps); q = q < 4 ? q + 1 : q < 8 ? q + 2 : q + q / 2) {
+        const long groups = tiles * q, a_round = 256 * r.fit, last = groups % a_round;
+        auto round = [&](long g) {
+          if (g == 0) return 0.f;
+          const int here = ceil_div(g, 256);
+          const float step = r.alone > r.full * here / r.fit ? r.alone : r.full * here / r.fit;
+          return step * ceil_div(steps, q) + r.ends;
+        };
+        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? 4.f + q * (float)m * n * 8.f / 5e6f : 0.f);
+        if (best < 0.f || t < best) { best = t; *kind = c; *splits = q; }
+      }
+    }
   };
   int one;
   choose(p->vocab, p->panel, p->dim_p, false, true, &p->cfg_z, &one);
   choose(p->dim, p->panel, p->vocab, true, true, &p->cfg_dh, &p->splits);
   choose(p->dim, p->vocab, p->panel, true, false, &p->cfg_dw, &p->splits_dw);
+  auto env = [](const char* n, int* v) { if (getenv(n)) *v = atoi(getenv(n)); };   // XX
+  env("VZ", &p->cfg_z); env("VH", &p->cfg_dh); env("VW", &p->cfg_dw); env("VHS", &p->splits); env("VWS", &p->splits_dw);   // XX
   if (p->panels > 1) p->splits_dw = 1;
   p->stat_cols = TILES[p->cfg_z].bm / TILES[p->cfg_z].wm;
   p->stats = ceil_div(p->vocab, TILES[p->cfg_z].bm) * TILES[p->cfg_z].wm;
