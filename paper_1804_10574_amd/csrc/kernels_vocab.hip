@@ -31,6 +31,7 @@ struct ProductArgs {
   void* e; long lde; float2* stat; int stats; const int* target; float* zt;   // stat: [N][stats], one of each wave's columns
   // epilogue 2: out[map[n]][m] = scale * sum + prev
   void* out; long ldo; int out_f32; const float* prev; long ldp; const float* scale; const int* map; size_t split_stride;
+  struct Total { const int* target; const float* row_loss; const float* weight; int T; float* loss; } total;   // loss null, or of one more workgroup
   int vec;                   // rows of `out` are pieces of a store: 16 bytes (OUT), 4 elements (SUM)
 };
 
@@ -151,6 +152,33 @@ template <typename T, int R, int KB, bool KC, int TILES> struct Reader {
   }
 };
 
+// The loss: the tokens' losses, weighted, in a fixed order and in 64 bits; by the threads of one workgroup
+template <int NT> __device__ __forceinline__ void total_loss(const ProductArgs::Total& a, unsigned char* smem) {
+  double* red = reinterpret_cast<double*>(smem);
+  int* n_red = reinterpret_cast<int*>(red + NT / 64);
+  const int tid = threadIdx.x;
+  double t = 0.0;
+  int n = 0;
+#pragma unroll 4
+  for (int i = tid; i < a.T; i += NT) {
+    const bool has = a.target[i] >= 0;
+    const float l = a.row_loss[i], w = a.weight ? a.weight[i] : 1.f;
+    t += has ? (double)l * w : 0.0;
+    n += has;
+  }
+  for (int k = 1; k < 64; k <<= 1) { t += __shfl_xor(t, k); n += __shfl_xor(n, k); }
+  if ((tid & 63) == 0) { red[tid >> 6] = t; n_red[tid >> 6] = n; }
+  __syncthreads();
+  if (tid) return;
+  t = 0.0; n = 0;
+  for (int i = 0; i < NT / 64; ++i) { t += red[i]; n += n_red[i]; }
+  *a.loss = (float)(a.weight ? t : t / (n > 0 ? n : 1));
+}
+__global__ __launch_bounds__(1024) void vocab_total_kernel(ProductArgs::Total a) {
+  __shared__ __align__(8) unsigned char smem[256];
+  total_loss<1024>(a, smem);
+}
+
 // Epilogues: EXP (product 1), OUT (results in the operands' type), SUM (through 32 bits: added to earlier sums, or left in fp32)
 enum { EXP = 1, OUT = 2, SUM = 3 };
 
@@ -182,6 +210,10 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
   }
   // Workgroups go to the 8 XCDs round-robin: each XCD gets a run of neighbouring tiles, in bands of 8 along n, which share operands in its L2
   const int tiles = a.tiles_m * a.tiles_n, total = tiles * a.splits, xcd = blockIdx.x & 7, q8 = total >> 3, r8 = total & 7;
+  if (EPI != EXP && blockIdx.x == (unsigned)total) {
+    total_loss<NT>(a.total, smem);
+    return;
+  }
   int id = q8 * xcd + (xcd < r8 ? xcd : r8) + (blockIdx.x >> 3);
   const int split = id / tiles;
   id -= split * tiles;
@@ -289,8 +321,12 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     for (int t = 0; t < AHEAD; ++t) if (k_lo + t < k_hi) request(t);
     unsigned stage = 0, next = AHEAD;
     for (int t = k_lo; t < k_hi; ++t) {
-      if (t + AHEAD < k_hi) {
-        step_barrier<(AHEAD - 1) * PER_STEP>();
+      if (STAGES == 1) {     // the stage is one workgroup's of several: they wait in turn
+        if (t > k_lo) lds_barrier();
+        request(0);
+        step_barrier<0>();
+      } else if (t + AHEAD < k_hi) {
+        step_barrier<(AHEAD > 0 ? AHEAD - 1 : 0) * PER_STEP>();
         request(next);
       } else {
         step_barrier<0>();
@@ -423,8 +459,12 @@ __device__ __forceinline__ float wave_total(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// Tokens with a target, in order: idx (their places), their targets, pos (place among them, -1 without one); their count, and what the products of
-// P are multiplied by in the end, in 32 bits: 1 / count, or the largest weight (P then holds weights relative to it: equal ones are not rounded). One workgroup.
+// What the products of P are multiplied by in the end, in 32 bits: 1 / count, or the largest weight (P then holds weights relative to it: equal ones are
+// not rounded)
+__device__ __forceinline__ float share_of(int count, bool weighted, float top) {
+  return !weighted ? 1.f / (float)(count > 0 ? count : 1) : top > 0x1p-100f && top < 0x1p100f ? top : 1.f;
+}
+// Tokens with a target, in order: idx (their places), their targets, pos (place among them, -1 without one); their count and share. One workgroup.
 __global__ __launch_bounds__(1024) void vocab_scan_kernel(const int* target, const float* weight, int T, int* idx, int* kept, int* pos, int* count, float* share) {
   __shared__ int s_wave[16];
   __shared__ float s_top[16];
@@ -455,34 +495,64 @@ __global__ __launch_bounds__(1024) void vocab_scan_kernel(const int* target, con
   if (tid) return;
   for (int i = 1; i < 16; ++i) top = fmaxf(top, s_top[i]);
   *count = before;
-  *share = !weight ? 1.f / (float)(before > 0 ? before : 1) : top > 0x1p-100f && top < 0x1p100f ? top : 1.f;
+  *share = share_of(before, weight != nullptr, top);
 }
 
 // A workgroup a row: row t of `from` to row pos[t] of `to` (pos null: t), widened to a whole number of 16-byte pieces with zeros. Without a place: the
-// token's results, which are zeros.
+// token's results, which are zeros. Scan: pos is not there yet; each workgroup counts the targets before its token, and leaves what the scan kernel would.
+struct Scan { const int* target; const float* weight; int T; int* idx; int* kept; int* count; float* share; };
+constexpr int SCAN_IN_GATHER = 2048;     // tokens: a workgroup reads up to 8 KB of targets, less than the 4 us that a launch before it takes
 template <typename T>
-__global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long ld, int dim, int dim_p, bool vec, const int* pos, T* to, T* dh, long ld_dh,
-                                                           float* row_loss, float* lse) {
+__global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long ld, int dim, int dim_p, bool vec, const int* pos, Scan scan, T* to, T* dh,
+                                                           long ld_dh, float* row_loss, float* lse) {
   constexpr int V = Store<T>::VEC;
-  const int t = blockIdx.x, j = pos ? pos[t] : t;
+  __shared__ int s_n[4];
+  __shared__ float s_top[4];
+  const int t = blockIdx.x, tid = threadIdx.x;
+  int j = t;
+  if (scan.target) {
+    const int y = scan.target[t];
+    const bool end = t == scan.T - 1;
+    int n = 0;
+    float top = 0.f;
+    for (int i = tid; i <= t; i += 256) {
+      const bool has = scan.target[i] >= 0;
+      n += has && i < t;
+      if (end && has && scan.weight) top = fmaxf(top, fabsf(scan.weight[i]));
+    }
+    for (int k = 1; k < 64; k <<= 1) { n += __shfl_xor(n, k); top = fmaxf(top, __shfl_xor(top, k)); }
+    if ((tid & 63) == 0) { s_n[tid >> 6] = n; s_top[tid >> 6] = top; }
+    __syncthreads();
+    n = s_n[0] + s_n[1] + s_n[2] + s_n[3];
+    j = y >= 0 ? n : -1;
+    if (tid == 0 && y >= 0) { scan.idx[j] = t; scan.kept[j] = y; }
+    if (tid == 0 && end) {
+      *scan.count = n + (y >= 0);
+      *scan.share = share_of(n + (y >= 0), scan.weight != nullptr, fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])));
+    }
+  } else if (pos) {
+    j = pos[t];
+  }
   if (j < 0) {
-    if (threadIdx.x == 0) { row_loss[t] = 0.f; if (lse) lse[t] = 0.f; }
-    if (dh) for (int c = threadIdx.x; c < dim; c += 256) dh[(size_t)t * ld_dh + c] = T{};
+    if (tid == 0) { row_loss[t] = 0.f; if (lse) lse[t] = 0.f; }
+    if (dh) for (int c = tid; c < dim; c += 256) dh[(size_t)t * ld_dh + c] = T{};
     return;
   }
   const T* in = from + (size_t)t * ld;
   T* out = to + (size_t)j * dim_p;
-  for (int c = threadIdx.x * V; c < dim_p; c += 256 * V) {
+  for (int c = tid * V; c < dim_p; c += 256 * V) {
+    uint4 q;
     if (vec) {
-      *reinterpret_cast<uint4*>(out + c) = *reinterpret_cast<const uint4*>(in + c);
+      q = *reinterpret_cast<const uint4*>(in + c);
+    } else if (c + V <= dim) {
+      __builtin_memcpy(&q, in + c, 16);
     } else {
       T e[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) e[i] = c + i < dim ? in[c + i] : T{};
-      uint4 q;
       __builtin_memcpy(&q, e, 16);
-      *reinterpret_cast<uint4*>(out + c) = q;
     }
+    *reinterpret_cast<uint4*>(out + c) = q;
   }
 }
 
@@ -548,6 +618,55 @@ __global__ __launch_bounds__(256) void vocab_row_kernel(RowArgs a) {
   }
 }
 
+// The same for the loss alone of a few tokens, and the loss, in one workgroup: as many waves a token as there are. (A launch for each of the two takes 4 us.)
+constexpr int FEW_ROWS = 16;
+__global__ __launch_bounds__(1024) void vocab_few_kernel(RowArgs a, int waves, float* loss) {
+  __shared__ float s_top[16], s_sum[16], s_loss[FEW_ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = wave / waves, first = (wave % waves) * 64 + lane, step = waves * 64;
+  float top = -__builtin_inff(), sum = 0.f;
+  if (r < a.rows) {
+    const float2* st = a.stat + (size_t)r * a.stats;
+    for (int i0 = first; i0 < a.stats; i0 += 8 * step) {       // 8 of them in flight, joined to what there is
+      float2 v[8];
+      float above = top;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * step;
+        v[k] = i < a.stats ? st[i] : make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) if (v[k].y != 0.f) above = fmaxf(above, v[k].x);
+      if (above == -__builtin_inff()) continue;
+      sum *= __expf(top - above);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) if (v[k].y != 0.f) sum += v[k].y * __expf(v[k].x - above);
+      top = above;
+    }
+    float all = top;
+    for (int k = 1; k < 64; k <<= 1) all = fmaxf(all, __shfl_xor(all, k));
+    sum = wave_total(top == -__builtin_inff() ? 0.f : sum * __expf(top - all));
+    if (lane == 0) { s_top[wave] = all; s_sum[wave] = sum; }
+  }
+  __syncthreads();
+  if (r < a.rows && wave % waves == 0 && lane == 0) {
+    for (int i = 0; i < waves; ++i) top = i ? fmaxf(top, s_top[wave + i]) : s_top[wave];
+    const float from = top == -__builtin_inff() ? 0.f : top;
+    sum = 0.f;
+    for (int i = 0; i < waves; ++i) sum += s_sum[wave + i] != 0.f ? s_sum[wave + i] * __expf(s_top[wave + i] - from) : 0.f;
+    const int y = a.target[r];
+    const float lse = from + logf(sum), l = y < 0 ? 0.f : lse - (y < a.V ? a.zt[r] : __builtin_nanf(""));
+    if (a.row_loss) a.row_loss[r] = l;
+    if (a.lse) a.lse[r] = y < 0 ? 0.f : lse;
+    s_loss[r] = l;
+  }
+  __syncthreads();
+  if (tid || !loss) return;
+  double t = 0.0;
+  int n = 0;
+  for (int i = 0; i < a.rows; ++i) if (a.target[i] >= 0) { t += (double)s_loss[i] * (a.weight ? a.weight[i] : 1.f); ++n; }
+  *loss = (float)(a.weight ? t : t / (n > 0 ? n : 1));
+}
+
 // dh from the parts of the vocabulary, or dw from those of the tokens, in their order
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_join_kernel(const float* part, int splits, size_t stride, int dim, const int* count, int first, int rows,
@@ -566,33 +685,12 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(const float* part, int 
   for (int e = 0; e < 4; ++e) if (c + e < dim) Store<T>::store1(out + e, v[e] * *scale);
 }
 
-// The loss: the tokens' losses, weighted, in a fixed order and in 64 bits. One workgroup.
-__global__ __launch_bounds__(1024) void vocab_total_kernel(const int* target, const float* row_loss, const float* weight, int T, float* loss) {
-  __shared__ double red[16];
-  __shared__ int n_red[16];
-  const int tid = threadIdx.x;
-  double t = 0.0;
-  int n = 0;
-  for (int i = tid; i < T; i += 1024) {
-    if (target[i] < 0) continue;
-    t += weight ? (double)row_loss[i] * weight[i] : (double)row_loss[i];
-    ++n;
-  }
-  for (int k = 1; k < 64; k <<= 1) { t += __shfl_xor(t, k); n += __shfl_xor(n, k); }
-  if ((tid & 63) == 0) { red[tid >> 6] = t; n_red[tid >> 6] = n; }
-  __syncthreads();
-  if (tid) return;
-  t = 0.0; n = 0;
-  for (int i = 0; i < 16; ++i) { t += red[i]; n += n_red[i]; }
-  *loss = (float)(weight ? t : t / (n > 0 ? n : 1));
-}
-
 // ---- launches ------------------------------------------------------------------------------------
 
 // Tiles of the products: rows along m (vocabulary or width) and n, waves along both, bytes of k in a stage, stages of LDS
-enum { LARGE, MEDIUM, SMALL, HALF, FEW, TILE_KINDS };
+enum { LARGE, MEDIUM, SHORT, SMALL, HALF, FEW, TILE_KINDS };
 struct Tile { int bm, bn, wm, wn, kb, stages; };
-constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 64, 4}, {128, 128, 2, 2, 128, 2}, {64, 64, 2, 2, 128, 3}, {128, 64, 4, 1, 128, 3}, {128, 32, 4, 1, 128, 4}};
+constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 64, 4}, {128, 128, 2, 2, 128, 2}, {128, 128, 2, 2, 128, 1}, {64, 64, 2, 2, 128, 3}, {128, 64, 4, 1, 128, 3}, {128, 32, 4, 1, 128, 4}};
 
 template <typename T, int KIND, bool AKC, bool BKC, int EPI>
 hipError_t product_run(ProductArgs a, hipStream_t s) {
@@ -604,7 +702,7 @@ hipError_t product_run(ProductArgs a, hipStream_t s) {
   a.tiles_m = (a.M + t.bm - 1) / t.bm;
   a.tiles_n = (a.N + t.bn - 1) / t.bn;
   if (a.tiles_n == 0) return hipSuccess;
-  DDG_LAUNCH(kernel, dim3(a.tiles_m * a.tiles_n * a.splits), dim3(t.wm * t.wn * 64), LDS, s, a);
+  DDG_LAUNCH(kernel, dim3(a.tiles_m * a.tiles_n * a.splits + (a.total.loss ? 1 : 0)), dim3(t.wm * t.wn * 64), LDS, s, a);
   return hipGetLastError();
 }
 
@@ -615,6 +713,7 @@ hipError_t product_any(const ProductArgs& a, int kind, hipStream_t s) {
     if (kind == FEW) return product_run<T, FEW, AKC, BKC, EPI>(a, s);
     if (kind == HALF) return product_run<T, HALF, AKC, BKC, EPI>(a, s);
   }
+  if constexpr (!BKC) if (kind == SHORT) return product_run<T, SHORT, AKC, BKC, EPI>(a, s);
   if (kind == SMALL) return product_run<T, SMALL, AKC, BKC, EPI>(a, s);
   return product_run<T, MEDIUM, AKC, BKC, EPI>(a, s);
 }
@@ -651,33 +750,34 @@ void vocab_plan(VocabPlan* p) {
   // The tiles, and for the sums of dh and dw (results of any size, long sums) the parts, that take the least time by what the kinds were measured at: us a
   // step of 128 bytes of k with one workgroup on a compute unit, with as many as fit, how many do, and us for the way in and out.
   struct Rate { float alone, full; int fit; float ends; };
-  static const Rate rates[2][TILE_KINDS] = {{{0.f, 0.f, 1, 0.f}, {2.0f, 4.1f, 2, 4.f}, {0.66f, 1.65f, 3, 3.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}},
-                                            {{1.0f, 1.45f, 1, 8.f}, {0.68f, 1.1f, 2, 4.f}, {0.28f, 0.7f, 3, 3.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}}};
-  auto choose = [&](long m, long n, long k, bool parts, bool few_ok, int* kind, int* splits) {
+  static const Rate rates[2][TILE_KINDS] = {
+      {{0.f, 0.f, 1, 0.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}},
+      {{1.0f, 1.45f, 1, 9.f}, {0.68f, 1.0f, 2, 4.f}, {1.3f, 1.35f, 3, 4.f}, {0.28f, 0.7f, 3, 2.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}}};
+  auto choose = [&](long m, long n, long k, bool parts, bool for_dw, int* kind, int* splits) {
     const long steps = ceil_div(k * (long)size, 128);
     float best = -1.f;
     *kind = MEDIUM; *splits = 1;
     for (int c = b16 ? LARGE : MEDIUM; c < TILE_KINDS; ++c) {
-      if (!few_ok && c > SMALL) break;
+      if (for_dw ? c > SMALL : c == SHORT) continue;
       const Rate r = rates[b16][c];
       const long tiles = (long)ceil_div(m, TILES[c].bm) * ceil_div(n, TILES[c].bn);
       for (int q = 1; q <= (parts ? 64 : 1) && (q == 1 || q * 2 <= steps); q = q < 4 ? q + 1 : q < 8 ? q + 2 : q + q / 2) {
         const long groups = tiles * q, a_round = 256 * r.fit, last = groups % a_round;
         auto round = [&](long g) {
           if (g == 0) return 0.f;
-          const int here = ceil_div(g, 256);
-          const float step = r.alone > r.full * here / r.fit ? r.alone : r.full * here / r.fit;
-          return step * ceil_div(steps, q) + r.ends;
+          const int here = ceil_div(g, 256);                  // workgroups on the fullest compute unit
+          const float crowded = r.fit == 1 ? r.full * g / 256 : r.full * here / r.fit;
+          return (r.alone > crowded ? r.alone : crowded) * ceil_div(steps, q) + r.ends;
         };
-        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? 4.f + q * (float)m * n * 8.f / 5e6f : 0.f);
+        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? 4.f + q * (float)m * n * 8.f / 1e7f : 0.f);
         if (best < 0.f || t < best) { best = t; *kind = c; *splits = q; }
       }
     }
   };
   int one;
-  choose(p->vocab, p->panel, p->dim_p, false, true, &p->cfg_z, &one);
-  choose(p->dim, p->panel, p->vocab, true, true, &p->cfg_dh, &p->splits);
-  choose(p->dim, p->vocab, p->panel, true, false, &p->cfg_dw, &p->splits_dw);
+  choose(p->vocab, p->panel, p->dim_p, false, false, &p->cfg_z, &one);
+  choose(p->dim, p->panel, p->vocab, true, false, &p->cfg_dh, &p->splits);
+  choose(p->dim, p->vocab, p->panel, true, true, &p->cfg_dw, &p->splits_dw);
   auto env = [](const char* n, int* v) { if (getenv(n)) *v = atoi(getenv(n)); };   // XX
   env("VZ", &p->cfg_z); env("VH", &p->cfg_dh); env("VW", &p->cfg_dw); env("VHS", &p->splits); env("VWS", &p->splits_dw);   // XX
   if (p->panels > 1) p->splits_dw = 1;
@@ -719,23 +819,28 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
   const T* h = (const T*)a.h; const T* w = (const T*)a.w;
   long ld_h = a.ld_h, ld_w = a.ld_w;
   if (p.pack_h) {
-    DDG_LAUNCH(vocab_scan_kernel, dim3(1), dim3(1024), 0, s, a.target, a.weight, p.tokens, idx, kept, pos, count, share);
-    TRY(hipGetLastError());
+    const bool alone = p.tokens == 0 || p.tokens > SCAN_IN_GATHER;
+    if (alone) {
+      DDG_LAUNCH(vocab_scan_kernel, dim3(1), dim3(1024), 0, s, a.target, a.weight, p.tokens, idx, kept, pos, count, share);
+      TRY(hipGetLastError());
+    }
     if (p.tokens) {
       const bool vec = p.dim == p.dim_p && (uintptr_t)a.h % 16 == 0 && ld_h * size % 16 == 0;
-      DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.tokens), dim3(256), 0, s, h, ld_h, p.dim, p.dim_p, vec, (const int*)pos, (T*)(a.ws + p.o_h), (T*)a.dh, a.ld_dh,
-                 row_loss, a.lse);
+      const Scan scan{alone ? nullptr : a.target, a.weight, p.tokens, idx, kept, count, share};
+      DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.tokens), dim3(256), 0, s, h, ld_h, p.dim, p.dim_p, vec, (const int*)pos, scan, (T*)(a.ws + p.o_h), (T*)a.dh,
+                 a.ld_dh, row_loss, a.lse);
       TRY(hipGetLastError());
     }
     h = (const T*)(a.ws + p.o_h); ld_h = p.dim_p;
   }
   if (p.pack_w) {
-    DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.vocab), dim3(256), 0, s, w, ld_w, p.dim, p.dim_p, false, (const int*)nullptr, (T*)(a.ws + p.o_w), (T*)nullptr, 0L,
+    DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.vocab), dim3(256), 0, s, w, ld_w, p.dim, p.dim_p, false, (const int*)nullptr, Scan{}, (T*)(a.ws + p.o_w), (T*)nullptr, 0L,
                (float*)nullptr, (float*)nullptr);
     TRY(hipGetLastError());
     w = (const T*)(a.ws + p.o_w); ld_w = p.dim_p;
   }
   const int* bound = p.pack_h ? count : nullptr;
+  ProductArgs::Total total{a.target, row_loss, a.weight, p.tokens, a.loss};   // left to the last panel's product of dh, or dw, if there is one
   for (int panel = 0; panel < p.panels; ++panel) {
     const int first = panel * p.panel, rows = p.tokens - first < p.panel ? p.tokens - first : p.panel;
     ProductArgs z{};
@@ -747,6 +852,10 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       RowArgs r{};
       r.stat = stat; r.stats = p.stats; r.stat_cols = p.stat_cols; r.zt = zt; r.target = z.target; r.idx = p.pack_h ? idx : nullptr; r.count = bound;
       r.weight = a.weight; r.share = share; r.first = first; r.rows = rows; r.V = p.vocab; r.row_loss = row_loss; r.lse = a.lse;
+      if (!p.pack_h && rows <= FEW_ROWS) {
+        DDG_LAUNCH(vocab_few_kernel, dim3(1), dim3(1024), 0, s, r, FEW_ROWS / rows, total.loss);
+        return hipGetLastError();
+      }
       int chunks = 1;
       if (p.grads) {
         r.p = a.ws + p.o_p; r.ld = p.ld_p;
@@ -767,6 +876,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       }
     }
     if (!p.grads) continue;
+    const bool last = panel + 1 == p.panels;
     // the parts of a sum, joined into rows `map` of `out`
     auto join = [&](const ProductArgs& g, int n, int splits, const int* limit, const int* map, int at, auto* out, long ld) -> hipError_t {
       for (int y = 0; y < n; y += 65535) {
@@ -781,6 +891,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       ProductArgs g{};
       g.A = w; g.lda = ld_w; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = rows; g.K = p.vocab; g.splits = p.splits;
       g.count = bound; g.first = first; g.dynamic = 1;
+      if (last) { g.total = total; total.loss = nullptr; }
       if (p.splits > 1) {
         g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)rows * g.ldo;
       } else {
@@ -793,6 +904,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       ProductArgs g{};
       g.A = h + (size_t)first * ld_h; g.lda = ld_h; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = p.vocab; g.K = rows; g.splits = p.splits_dw;
       g.count = bound; g.first = first; g.dynamic = 2;
+      if (last) { g.total = total; total.loss = nullptr; }
       if (p.splits_dw > 1) {
         g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)p.vocab * g.ldo;
         TRY((product_out<T, false, false>(g, p.dim, p.cfg_dw, s)));
@@ -800,7 +912,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
         else TRY(join(g, p.vocab, p.splits_dw, nullptr, nullptr, 0, (T*)a.dw, a.ld_dw));
         continue;
       }
-      const bool f32 = size == 4 || p.dw_f32, last = panel + 1 == p.panels;
+      const bool f32 = size == 4 || p.dw_f32;
       float* sum = p.acc ? (float*)(a.ws + p.o_acc) : (float*)a.dw;
       const long ld_sum = p.acc ? (long)up(p.dim, 4) : a.ld_dw;
       if (panel) { g.prev = sum; g.ldp = ld_sum; }
@@ -810,8 +922,8 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       TRY((product_out<T, false, false>(g, p.dim, p.cfg_dw, s)));
     }
   }
-  if (a.loss) {
-    DDG_LAUNCH(vocab_total_kernel, dim3(1), dim3(1024), 0, s, a.target, (const float*)row_loss, a.weight, p.tokens, a.loss);
+  if (total.loss) {
+    DDG_LAUNCH(vocab_total_kernel, dim3(1), dim3(1024), 0, s, total);
     TRY(hipGetLastError());
   }
   return hipSuccess;
