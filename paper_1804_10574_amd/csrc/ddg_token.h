@@ -36,14 +36,15 @@ struct VocabPlan {
   int tokens, dim, vocab, dtype;
   bool grads, dw_f32;
   bool pack_h, pack_w;       // operands whose rows are not 16-byte pieces are copied to ones that are
-  int dim_p;                 // their width then
+  bool planes;               // fp32 operands are taken apart into three bf16 planes each
+  int dim_p;                 // width of the copies
   int panel, panels;         // tokens of a panel
   long ld_p;                 // elements between the rows of the panel's probabilities
   int cfg_z, cfg_dh, cfg_dw; // tiles of the three products
   int stat_cols, stats;      // columns that share a maximum and sum, and their number
   int splits, splits_dw;     // parts of the vocabulary that dh is summed over, of the tokens that dw is
   bool acc;                  // dw is summed over panels in a buffer of the workspace
-  size_t o_scalar, o_row, o_zt, o_stat, o_p, o_part, o_acc, o_h, o_w, bytes;
+  size_t o_scalar, o_row, o_zt, o_stat, o_p, o_planes, o_part, o_acc, o_h, o_w, bytes;
 };
 struct VocabArgs {
   const void* h; const void* w; const int32_t* target; const float* weight;

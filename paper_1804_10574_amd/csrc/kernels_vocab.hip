@@ -10,7 +10,6 @@
 #include "ddg_token.h"
 
 #include <type_traits>
-#include <stdlib.h>
 
 namespace ddg {
 namespace {
@@ -23,6 +22,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 struct ProductArgs {
   const void* A; const void* B;
   long lda, ldb;
+  long plane_a, plane_b;     // SPLIT: bytes from one of an operand's three planes to the next
   int M, N, K;               // K: 16-byte pieces of a KC operand start below it; the other kind's rows end there
   const int* count;          // tokens left over the panels, or null: `dynamic` says which of N (1) and K (2) they bound
   int first, dynamic;        // first token of the panel
@@ -179,20 +179,24 @@ __global__ __launch_bounds__(1024) void vocab_total_kernel(ProductArgs::Total a)
   total_loss<1024>(a, smem);
 }
 
+// fp32 operands as three bf16 each, x = x0 + x1 + x2 with 8 bits apiece: the six products of two planes that reach 2^-24 of the whole (the others are
+// smaller than the rounding of an fp32 product), the smallest first. Six passes at the bf16 rate are nearly twice as fast as one on the fp32 matrix instructions.
+__device__ constexpr int PLANES[6][2] = {{2, 0}, {1, 1}, {0, 2}, {1, 0}, {0, 1}, {0, 0}};
+
 // Epilogues: EXP (product 1), OUT (results in the operands' type), SUM (through 32 bits: added to earlier sums, or left in fp32)
 enum { EXP = 1, OUT = 2, SUM = 3 };
 
-template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, int EPI> struct ProductShape {
-  typedef std::conditional_t<EPI == SUM, float, T> Staged;
+template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, int EPI, bool SPLIT> struct ProductShape {
+  typedef std::conditional_t<EPI == SUM || SPLIT, float, T> Staged;
   static constexpr int NT = WM * WN * 64, STAGE = (BM + BN) * KB;
   // the tile on its way out: 32 rows of each wave column at a time, rows 16 bytes apart in the banks
   static constexpr int PITCH = BM * (int)sizeof(Staged) + 16, LEAVING = WN * 32 * PITCH;
   static constexpr int LDS = STAGES * STAGE > LEAVING ? STAGES * STAGE : LEAVING;
 };
 
-template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool AKC, bool BKC, int EPI>
+template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
 __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
-  typedef ProductShape<T, BM, BN, WM, WN, KB, STAGES, EPI> Shape;
+  typedef ProductShape<T, BM, BN, WM, WN, KB, STAGES, EPI, SPLIT> Shape;
   constexpr int NT = Shape::NT, MT = BM / WM / 32, NTL = BN / WN / 32, BK = KB / (int)sizeof(T), STEPS = KB / 32, STAGE = Shape::STAGE;
   constexpr bool INTERLEAVED = MT * NTL >= 8;
   typedef Operand<T, BM, KB, AKC, NT> OpA;
@@ -250,22 +254,30 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
   constexpr int PER_STEP = OpA::LOADS + OpB::LOADS, AHEAD = STAGES - 1;
-  auto load = [&](int t, unsigned stage) __attribute__((always_inline)) {
+  auto load = [&](int left, unsigned stage) __attribute__((always_inline)) {
     const u32x4 res_a = resource(la.base), res_b = resource(lb.base);
 #pragma unroll
-    for (int j = 0; j < OpA::LOADS; ++j) la.load(res_a, lds + stage * STAGE, wave, K - t * BK, j);
+    for (int j = 0; j < OpA::LOADS; ++j) la.load(res_a, lds + stage * STAGE, wave, left, j);
 #pragma unroll
-    for (int j = 0; j < OpB::LOADS; ++j) lb.load(res_b, lds + stage * STAGE + OpA::BYTES, wave, K - t * BK, j);
-    la.step(); lb.step();
+    for (int j = 0; j < OpB::LOADS; ++j) lb.load(res_b, lds + stage * STAGE + OpA::BYTES, wave, left, j);
   };
-  int at_k = k_lo + turn;    // the next step that is requested: the first one is `turn`, after the last comes k_lo
-  auto request = [&](unsigned stage) __attribute__((always_inline)) {
-    load(at_k, stage);
+  // To the next step that is requested: the first one is `turn`, after the last comes k_lo (SPLIT: of the next pair of planes)
+  constexpr int PAIRS = SPLIT ? 6 : 1;
+  int at_k = k_lo + turn, pair = 0;
+  if (SPLIT) { la.base += PLANES[0][0] * a.plane_a; lb.base += PLANES[0][1] * a.plane_b; }
+  auto ahead = [&]() __attribute__((always_inline)) {
+    la.step(); lb.step();
     if (++at_k == k_hi) {
       at_k = k_lo;
       la.base -= (k_hi - k_lo) * la.advance; lb.base -= (k_hi - k_lo) * lb.advance;
+      if (SPLIT && pair < PAIRS - 1) {
+        la.base += (PLANES[pair + 1][0] - PLANES[pair][0]) * a.plane_a;
+        lb.base += (PLANES[pair + 1][1] - PLANES[pair][1]) * a.plane_b;
+        ++pair;
+      }
     }
   };
+  auto request = [&](unsigned stage) __attribute__((always_inline)) { load(K - at_k * BK, stage); ahead(); };
   if constexpr (INTERLEAVED) {
     // The matrix instructions of a step in a row, and one LDS read of the next k's fragments or one load between each two: a wave never has a burst of
     // others to issue first (product 2 of 4096 tokens of 131072 entries and width 4096: 3.06 ms, 3.29 with the waves in two groups that take turns at LDS and the matrix
@@ -273,7 +285,10 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     // step's loads are waited for. Step t requests step t + AHEAD into the stage of step t - 1. Loads past the end of k are made, and write zeros: the counts are constant.
     static_assert(STAGES >= 3 && PER_STEP % STEPS == 0, "");
 #pragma unroll
-    for (int t = 0; t < AHEAD; ++t) load(k_lo + t, t);
+    for (int t = 0; t < AHEAD; ++t) {
+      load(t < (k_hi - k_lo) * PAIRS ? K - at_k * BK : 0, t);
+      ahead();
+    }
     typename Frag<T>::t fa[2][MT], fb[2][NTL];
     step_barrier<(AHEAD - 1) * PER_STEP>();
 #pragma unroll
@@ -281,10 +296,11 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
 #pragma unroll
     for (int j = 0; j < NTL; ++j) fb[0][j] = rb.get(smem + OpA::BYTES, j, 0);
     unsigned stage = 0, before = STAGES - 1;
-    for (int t = k_lo; t < k_hi; ++t) {
+    const int steps = (k_hi - k_lo) * PAIRS;
+    for (int t = 0; t < steps; ++t) {
       const unsigned next = stage == STAGES - 1 ? 0 : stage + 1, fill = lds + before * STAGE;
       const u32x4 res_a = resource(la.base), res_b = resource(lb.base);
-      const int left = K - (t + AHEAD) * BK;
+      const int left = t + AHEAD < steps ? K - at_k * BK : 0;
 #pragma unroll
       for (int s = 0; s < STEPS; ++s) {
         const bool last = s == STEPS - 1;
@@ -309,7 +325,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      la.step(); lb.step();
+      ahead();
       before = stage;
       stage = next;
     }
@@ -391,7 +407,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
       if (!a.e) continue;
     }
     typedef typename Shape::Staged S;
-    constexpr int V = EPI == SUM ? 4 : 16 / (int)sizeof(T), PIECES = BM / V, ROWS = WN * 32;
+    constexpr int V = 16 / (int)sizeof(S), PIECES = BM / V, ROWS = WN * 32;
     float4 prev[EPI == SUM ? ROWS * PIECES / NT : 1];
     if (EPI == SUM && a.prev) {          // requested before the tile goes through LDS
 #pragma unroll
@@ -419,7 +435,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
       if (n >= N) continue;
       const S* from = reinterpret_cast<const S*>(smem + r * Shape::PITCH) + c * V;
       if (EPI == EXP) {
-        if (m < a.lde) *reinterpret_cast<uint4*>((T*)a.e + (size_t)n * a.lde + m) = *reinterpret_cast<const uint4*>(from);
+        if (m < a.lde) *reinterpret_cast<uint4*>((S*)a.e + (size_t)n * a.lde + m) = *reinterpret_cast<const uint4*>(from);
         continue;
       }
       if (m >= a.M) continue;
@@ -498,13 +514,25 @@ __global__ __launch_bounds__(1024) void vocab_scan_kernel(const int* target, con
   *share = share_of(before, weight != nullptr, top);
 }
 
+// The planes of four fp32 values, each the rounding of what the earlier ones left
+__device__ __forceinline__ void split4(float4 v, uint2 (&p)[3]) {
+  float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = make_uint2(f32x2_to_bf16x2(f[0], f[1]), f32x2_to_bf16x2(f[2], f[3]));
+    f[0] -= __uint_as_float(p[i].x << 16); f[1] -= __uint_as_float(p[i].x & 0xffff0000u);
+    f[2] -= __uint_as_float(p[i].y << 16); f[3] -= __uint_as_float(p[i].y & 0xffff0000u);
+  }
+}
+
 // A workgroup a row: row t of `from` to row pos[t] of `to` (pos null: t), widened to a whole number of 16-byte pieces with zeros. Without a place: the
 // token's results, which are zeros. Scan: pos is not there yet; each workgroup counts the targets before its token, and leaves what the scan kernel would.
+// SPLIT: to three planes of bf16, `plane` elements apart.
 struct Scan { const int* target; const float* weight; int T; int* idx; int* kept; int* count; float* share; };
 constexpr int SCAN_IN_GATHER = 2048;     // tokens: a workgroup reads up to 8 KB of targets, less than the 4 us that a launch before it takes
-template <typename T>
-__global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long ld, int dim, int dim_p, bool vec, const int* pos, Scan scan, T* to, T* dh,
-                                                           long ld_dh, float* row_loss, float* lse) {
+template <typename T, bool SPLIT>
+__global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long ld, int dim, int dim_p, bool vec, const int* pos, Scan scan, void* to_any,
+                                                           size_t plane, T* dh, long ld_dh, float* row_loss, float* lse) {
   constexpr int V = Store<T>::VEC;
   __shared__ int s_n[4];
   __shared__ float s_top[4];
@@ -539,7 +567,6 @@ __global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long l
     return;
   }
   const T* in = from + (size_t)t * ld;
-  T* out = to + (size_t)j * dim_p;
   for (int c = tid * V; c < dim_p; c += 256 * V) {
     uint4 q;
     if (vec) {
@@ -552,7 +579,14 @@ __global__ __launch_bounds__(256) void vocab_gather_kernel(const T* from, long l
       for (int i = 0; i < V; ++i) e[i] = c + i < dim ? in[c + i] : T{};
       __builtin_memcpy(&q, e, 16);
     }
-    *reinterpret_cast<uint4*>(out + c) = q;
+    if constexpr (SPLIT) {
+      uint2 planes[3];
+      split4(__builtin_bit_cast(float4, q), planes);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>((bf16_t*)to_any + i * plane + (size_t)j * dim_p + c) = planes[i];
+    } else {
+      *reinterpret_cast<uint4*>((T*)to_any + (size_t)j * dim_p + c) = q;
+    }
   }
 }
 
@@ -562,6 +596,7 @@ struct RowArgs {
   int first, rows, V;
   float* row_loss; float* lse;
   void* p; long ld; int chunk;       // gradients: exp(z - m), turned into P; columns of a workgroup
+  bf16_t* planes; size_t plane;      // or P goes here, in three planes
 };
 
 // The log-sum of a token from its maxima and sums, its loss, and its row of P: a workgroup takes a chunk of the row (blockIdx.x), each of
@@ -613,6 +648,15 @@ __global__ __launch_bounds__(256) void vocab_row_kernel(RowArgs a) {
     for (int e = 0; e < V; ++e) {
       v[e] = c + e < a.V ? v[e] * scale : 0.f;
       if (c + e == y) v[e] = (__expf(zt - from) / sum - 1.f) * share;
+    }
+    if constexpr (sizeof(T) == 4) {
+      if (a.planes) {
+        uint2 planes[3];
+        split4(make_float4(v[0], v[1], v[2], v[3]), planes);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(a.planes + i * a.plane + (size_t)r * a.ld + c) = planes[i];
+        continue;
+      }
     }
     Store<T>::store_vec(row + c, v);
   }
@@ -675,6 +719,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(const float* part, int 
   if (c >= dim || (count && first + r >= *count)) return;
   const int wide = (dim + 3) & ~3;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
   for (int s = 0; s < splits; ++s) {
     const float4 q = *reinterpret_cast<const float4*>(part + s * stride + (size_t)r * wide + c);
     v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
@@ -692,11 +737,11 @@ enum { LARGE, MEDIUM, SHORT, SMALL, HALF, FEW, TILE_KINDS };
 struct Tile { int bm, bn, wm, wn, kb, stages; };
 constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 64, 4}, {128, 128, 2, 2, 128, 2}, {128, 128, 2, 2, 128, 1}, {64, 64, 2, 2, 128, 3}, {128, 64, 4, 1, 128, 3}, {128, 32, 4, 1, 128, 4}};
 
-template <typename T, int KIND, bool AKC, bool BKC, int EPI>
+template <typename T, int KIND, bool AKC, bool BKC, int EPI, bool SPLIT = false>
 hipError_t product_run(ProductArgs a, hipStream_t s) {
   constexpr Tile t = TILES[KIND];
-  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, EPI>::LDS;
-  const auto kernel = &product_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, AKC, BKC, EPI>;
+  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, EPI, SPLIT>::LDS;
+  const auto kernel = &product_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, AKC, BKC, EPI, SPLIT>;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return attr;
   a.tiles_m = (a.M + t.bm - 1) / t.bm;
@@ -708,6 +753,7 @@ hipError_t product_run(ProductArgs a, hipStream_t s) {
 
 template <typename T, bool AKC, bool BKC, int EPI>
 hipError_t product_any(const ProductArgs& a, int kind, hipStream_t s) {
+  if constexpr (sizeof(T) == 4) if (kind == LARGE) return product_run<bf16_t, LARGE, AKC, BKC, EPI, true>(a, s);   // three planes an operand
   if constexpr (sizeof(T) == 2) if (kind == LARGE) return product_run<T, LARGE, AKC, BKC, EPI>(a, s);
   if constexpr (BKC) {
     if (kind == FEW) return product_run<T, FEW, AKC, BKC, EPI>(a, s);
@@ -724,7 +770,8 @@ template <typename T, bool AKC, bool BKC> hipError_t product_out(ProductArgs a, 
   a.vec = dim % piece == 0 && (uintptr_t)a.out % bytes == 0 && a.ldo % piece == 0 && a.split_stride % piece == 0 &&
           (!a.prev || ((uintptr_t)a.prev % 16 == 0 && a.ldp % 4 == 0));
   a.out_f32 = a.out_f32 || sizeof(T) == 4;
-  return sum ? product_any<T, AKC, BKC, SUM>(a, kind, s) : product_any<T, AKC, BKC, OUT>(a, kind, s);
+  if constexpr (sizeof(T) == 4) return product_any<T, AKC, BKC, SUM>(a, kind, s);
+  else return sum ? product_any<T, AKC, BKC, SUM>(a, kind, s) : product_any<T, AKC, BKC, OUT>(a, kind, s);
 }
 
 size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
@@ -737,31 +784,25 @@ constexpr size_t PANEL_BYTES = ((size_t)1 << 30) + ((size_t)1 << 24);    // of a
 void vocab_plan(VocabPlan* p) {
   const size_t size = dtype_size(p->dtype);
   const int vec = 16 / (int)size;
-  p->dim_p = (int)up(p->dim, vec);
-  p->ld_p = (long)up(p->vocab, 64) + 64;           // (rows an odd number of 128 bytes apart where the vocabulary is a power of two)
-  p->pack_h = p->grads || p->pack_h || p->tokens > 64;
-  const size_t row = p->grads ? p->ld_p * size : (size_t)p->vocab / 4 + 64;
-  long most = (long)(PANEL_BYTES / row / 256 * 256);
-  if (most < 256) most = 256;
-  p->panels = p->tokens > most ? ceil_div(p->tokens, most) : 1;
-  p->panel = p->panels > 1 ? (int)up(ceil_div(p->tokens, p->panels), 256) : p->tokens;
-  if (p->panels > 1) p->panels = ceil_div(p->tokens, p->panel);
   const bool b16 = size == 2;
   // The tiles, and for the sums of dh and dw (results of any size, long sums) the parts, that take the least time by what the kinds were measured at: us a
-  // step of 128 bytes of k with one workgroup on a compute unit, with as many as fit, how many do, and us for the way in and out.
+  // step of 128 bytes of k with one workgroup on a compute unit, with as many as fit, how many do, and us for the way in and out. fp32 in the largest tiles
+  // is in planes: six steps of bf16, of half as many bytes.
   struct Rate { float alone, full; int fit; float ends; };
   static const Rate rates[2][TILE_KINDS] = {
-      {{0.f, 0.f, 1, 0.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}},
+      {{3.2f, 4.6f, 1, 14.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}},
       {{1.0f, 1.45f, 1, 9.f}, {0.68f, 1.0f, 2, 4.f}, {1.3f, 1.35f, 3, 4.f}, {0.28f, 0.7f, 3, 2.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}}};
-  auto choose = [&](long m, long n, long k, bool parts, bool for_dw, int* kind, int* splits) {
+  enum Sum { LOGITS, DH, DW };
+  auto choose = [&](Sum sum, int tokens, int from, int to, int* kind, int* splits) {
+    const long m = sum == LOGITS ? p->vocab : p->dim, n = sum == DW ? p->vocab : tokens, k = sum == LOGITS ? p->dim : sum == DH ? p->vocab : tokens;
     const long steps = ceil_div(k * (long)size, 128);
     float best = -1.f;
-    *kind = MEDIUM; *splits = 1;
-    for (int c = b16 ? LARGE : MEDIUM; c < TILE_KINDS; ++c) {
-      if (for_dw ? c > SMALL : c == SHORT) continue;
+    *kind = from; *splits = 1;
+    for (int c = from; c < to; ++c) {
+      if (sum == DW ? c > SMALL : c == SHORT) continue;
       const Rate r = rates[b16][c];
       const long tiles = (long)ceil_div(m, TILES[c].bm) * ceil_div(n, TILES[c].bn);
-      for (int q = 1; q <= (parts ? 64 : 1) && (q == 1 || q * 2 <= steps); q = q < 4 ? q + 1 : q < 8 ? q + 2 : q + q / 2) {
+      for (int q = 1; q <= (sum == LOGITS ? 1 : 64) && (q == 1 || q * 2 <= steps); q = q < 4 ? q + 1 : q < 8 ? q + 2 : q + q / 2) {
         const long groups = tiles * q, a_round = 256 * r.fit, last = groups % a_round;
         auto round = [&](long g) {
           if (g == 0) return 0.f;
@@ -769,17 +810,37 @@ void vocab_plan(VocabPlan* p) {
           const float crowded = r.fit == 1 ? r.full * g / 256 : r.full * here / r.fit;
           return (r.alone > crowded ? r.alone : crowded) * ceil_div(steps, q) + r.ends;
         };
-        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? 4.f + q * (float)m * n * 8.f / 1e7f : 0.f);
+        const float bytes = q * (float)m * n * 8.f;           // partial sums, written and read; up to 256 MB of them stay in the last cache
+        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? 4.f + bytes / (bytes < 2.4e8f ? 1e7f : 5e6f) : 0.f);
         if (best < 0.f || t < best) { best = t; *kind = c; *splits = q; }
       }
     }
+    return best;
   };
-  int one;
-  choose(p->vocab, p->panel, p->dim_p, false, false, &p->cfg_z, &one);
-  choose(p->dim, p->panel, p->vocab, true, false, &p->cfg_dh, &p->splits);
-  choose(p->dim, p->vocab, p->panel, true, true, &p->cfg_dw, &p->splits_dw);
-  auto env = [](const char* n, int* v) { if (getenv(n)) *v = atoi(getenv(n)); };   // XX
-  env("VZ", &p->cfg_z); env("VH", &p->cfg_dh); env("VW", &p->cfg_dw); env("VHS", &p->splits); env("VWS", &p->splits_dw);   // XX
+  auto choose_all = [&](int tokens, int from, int to) {
+    int one;
+    float t = choose(LOGITS, tokens, from, to, &p->cfg_z, &one);
+    if (p->grads) t += choose(DH, tokens, from, to, &p->cfg_dh, &p->splits) + choose(DW, tokens, from, to, &p->cfg_dw, &p->splits_dw);
+    return t;
+  };
+  p->splits = p->splits_dw = 1;
+  p->planes = false;
+  if (!b16) {                                        // planes: 10 bytes moved for an element of h and w, 8 for one of P
+    const float moved = 10.f * p->dim * ((float)p->vocab + p->tokens) + (p->grads ? 8.f * p->tokens * p->vocab : 0.f);
+    const float direct = choose_all(p->tokens, MEDIUM, TILE_KINDS);
+    p->planes = choose_all(p->tokens, LARGE, MEDIUM) + moved / 4.5e6f + 5.f < direct;
+  }
+  p->dim_p = (int)up(p->dim, p->planes ? 8 : vec);
+  if (p->planes) p->pack_h = p->pack_w = true;
+  p->ld_p = (long)up(p->vocab, 64) + 64;           // (rows an odd number of 128 bytes apart where the vocabulary is a power of two)
+  p->pack_h = p->grads || p->pack_h || p->tokens > 64;
+  const size_t row = p->grads ? p->ld_p * (p->planes ? 10 : size) : (size_t)p->vocab / 4 + 64;
+  long most = (long)(PANEL_BYTES / row / 256 * 256);
+  if (most < 256) most = 256;
+  p->panels = p->tokens > most ? ceil_div(p->tokens, most) : 1;
+  p->panel = p->panels > 1 ? (int)up(ceil_div(p->tokens, p->panels), 256) : p->tokens;
+  if (p->panels > 1) p->panels = ceil_div(p->tokens, p->panel);
+  choose_all(p->panel, p->planes || b16 ? LARGE : MEDIUM, p->planes ? MEDIUM : TILE_KINDS);
   if (p->panels > 1) p->splits_dw = 1;
   p->stat_cols = TILES[p->cfg_z].bm / TILES[p->cfg_z].wm;
   p->stats = ceil_div(p->vocab, TILES[p->cfg_z].bm) * TILES[p->cfg_z].wm;
@@ -792,11 +853,13 @@ void vocab_plan(VocabPlan* p) {
   p->o_zt = take(T * 4);
   p->o_stat = take((size_t)p->panel * p->stats * 8);
   p->o_p = p->grads ? take((size_t)p->panel * p->ld_p * size) : 0;
+  p->o_planes = p->grads && p->planes ? take((size_t)p->panel * p->ld_p * 6) : 0;
+  const size_t operand = p->planes ? 6 : size;
   const size_t part = p->splits > 1 ? (size_t)p->splits * p->panel : 0, part_dw = p->splits_dw > 1 ? (size_t)p->splits_dw * p->vocab : 0;
   p->o_part = p->grads ? take((part > part_dw ? part : part_dw) * up(p->dim, 4) * 4) : 0;
   p->o_acc = p->acc ? take((size_t)p->vocab * up(p->dim, 4) * 4) : 0;
-  p->o_h = p->pack_h ? take(T * p->dim_p * size) : 0;
-  p->o_w = p->pack_w ? take((size_t)p->vocab * p->dim_p * size) : 0;
+  p->o_h = p->pack_h ? take(T * p->dim_p * operand) : 0;
+  p->o_w = p->pack_w ? take((size_t)p->vocab * p->dim_p * operand) : 0;
   p->bytes = at;
 }
 
@@ -816,8 +879,20 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
   float* row_loss = a.row_loss ? a.row_loss : (float*)(pos + p.tokens);
   float* zt = (float*)(a.ws + p.o_zt);
   float2* stat = (float2*)(a.ws + p.o_stat);
-  const T* h = (const T*)a.h; const T* w = (const T*)a.w;
+  const unsigned char* h = (const unsigned char*)a.h;
+  const void* w = a.w;
   long ld_h = a.ld_h, ld_w = a.ld_w;
+  const size_t operand = p.planes ? 2 : size;                       // bytes of an element of a product's operands
+  const size_t plane_h = (size_t)p.tokens * p.dim_p, plane_w = (size_t)p.vocab * p.dim_p, plane_p = (size_t)p.panel * p.ld_p;
+  auto gather = [&](const T* from, long ld, int n, bool vec, const Scan& scan, const int* at, void* to, size_t plane, T* dh) {
+    if constexpr (sizeof(T) == 4) {
+      if (p.planes) {
+        DDG_LAUNCH((vocab_gather_kernel<T, true>), dim3(n), dim3(256), 0, s, from, ld, p.dim, p.dim_p, vec, at, scan, to, plane, dh, a.ld_dh, row_loss, a.lse);
+        return;
+      }
+    }
+    DDG_LAUNCH((vocab_gather_kernel<T, false>), dim3(n), dim3(256), 0, s, from, ld, p.dim, p.dim_p, vec, at, scan, to, plane, dh, a.ld_dh, row_loss, a.lse);
+  };
   if (p.pack_h) {
     const bool alone = p.tokens == 0 || p.tokens > SCAN_IN_GATHER;
     if (alone) {
@@ -827,24 +902,23 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
     if (p.tokens) {
       const bool vec = p.dim == p.dim_p && (uintptr_t)a.h % 16 == 0 && ld_h * size % 16 == 0;
       const Scan scan{alone ? nullptr : a.target, a.weight, p.tokens, idx, kept, count, share};
-      DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.tokens), dim3(256), 0, s, h, ld_h, p.dim, p.dim_p, vec, (const int*)pos, scan, (T*)(a.ws + p.o_h), (T*)a.dh,
-                 a.ld_dh, row_loss, a.lse);
+      gather((const T*)a.h, a.ld_h, p.tokens, vec, scan, (const int*)pos, a.ws + p.o_h, plane_h, (T*)a.dh);
       TRY(hipGetLastError());
     }
-    h = (const T*)(a.ws + p.o_h); ld_h = p.dim_p;
+    h = a.ws + p.o_h; ld_h = p.dim_p;
   }
   if (p.pack_w) {
-    DDG_LAUNCH(vocab_gather_kernel<T>, dim3(p.vocab), dim3(256), 0, s, w, ld_w, p.dim, p.dim_p, false, (const int*)nullptr, Scan{}, (T*)(a.ws + p.o_w), (T*)nullptr, 0L,
-               (float*)nullptr, (float*)nullptr);
+    const bool vec = p.dim == p.dim_p && (uintptr_t)a.w % 16 == 0 && ld_w * size % 16 == 0;
+    gather((const T*)a.w, a.ld_w, p.vocab, vec, Scan{}, (const int*)nullptr, a.ws + p.o_w, plane_w, (T*)nullptr);
     TRY(hipGetLastError());
-    w = (const T*)(a.ws + p.o_w); ld_w = p.dim_p;
+    w = a.ws + p.o_w; ld_w = p.dim_p;
   }
   const int* bound = p.pack_h ? count : nullptr;
   ProductArgs::Total total{a.target, row_loss, a.weight, p.tokens, a.loss};   // left to the last panel's product of dh, or dw, if there is one
   for (int panel = 0; panel < p.panels; ++panel) {
     const int first = panel * p.panel, rows = p.tokens - first < p.panel ? p.tokens - first : p.panel;
     ProductArgs z{};
-    z.A = w; z.lda = ld_w; z.B = h + (size_t)first * ld_h; z.ldb = ld_h; z.M = p.vocab; z.N = rows; z.K = p.dim_p; z.splits = 1;
+    z.A = w; z.lda = ld_w; z.B = h + (size_t)first * ld_h * operand; z.ldb = ld_h; z.plane_a = plane_w * 2; z.plane_b = plane_h * 2; z.M = p.vocab; z.N = rows; z.K = p.dim_p; z.splits = 1;
     z.count = bound; z.first = first; z.dynamic = 1;
     z.e = p.grads ? a.ws + p.o_p : nullptr; z.lde = p.ld_p; z.stat = stat; z.stats = p.stats; z.target = p.pack_h ? kept : a.target; z.zt = zt;
     TRY((product_any<T, true, true, EXP>(z, p.cfg_z, s)));
@@ -859,6 +933,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       int chunks = 1;
       if (p.grads) {
         r.p = a.ws + p.o_p; r.ld = p.ld_p;
+        if (p.planes) { r.planes = (bf16_t*)(a.ws + p.o_planes); r.plane = plane_p; }
         // enough workgroups to fill the chip, none with less than two trips
         const int unit = 2 * 256 * Store<T>::VEC, most = ceil_div(p.ld_p, unit);
         chunks = ceil_div(2048, rows);
@@ -871,12 +946,14 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
         const int n = rows - y < 65535 ? rows - y : 65535;
         q.first += y; q.stat += (size_t)y * q.stats; q.rows = n;
         if (q.p) q.p = (T*)q.p + (size_t)y * q.ld;
+        if (q.planes) q.planes += (size_t)y * q.ld;
         DDG_LAUNCH(vocab_row_kernel<T>, dim3(chunks, n), dim3(256), 0, s, q);
         TRY(hipGetLastError());
       }
     }
     if (!p.grads) continue;
     const bool last = panel + 1 == p.panels;
+    const void* probs = a.ws + (p.planes ? p.o_planes : p.o_p);
     // the parts of a sum, joined into rows `map` of `out`
     auto join = [&](const ProductArgs& g, int n, int splits, const int* limit, const int* map, int at, auto* out, long ld) -> hipError_t {
       for (int y = 0; y < n; y += 65535) {
@@ -889,7 +966,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
     };
     if (a.dh && rows) {
       ProductArgs g{};
-      g.A = w; g.lda = ld_w; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = rows; g.K = p.vocab; g.splits = p.splits;
+      g.A = w; g.lda = ld_w; g.B = probs; g.ldb = p.ld_p; g.plane_a = plane_w * 2; g.plane_b = plane_p * 2; g.M = p.dim; g.N = rows; g.K = p.vocab; g.splits = p.splits;
       g.count = bound; g.first = first; g.dynamic = 1;
       if (last) { g.total = total; total.loss = nullptr; }
       if (p.splits > 1) {
@@ -902,7 +979,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
     }
     if (a.dw) {
       ProductArgs g{};
-      g.A = h + (size_t)first * ld_h; g.lda = ld_h; g.B = a.ws + p.o_p; g.ldb = p.ld_p; g.M = p.dim; g.N = p.vocab; g.K = rows; g.splits = p.splits_dw;
+      g.A = h + (size_t)first * ld_h * operand; g.lda = ld_h; g.B = probs; g.ldb = p.ld_p; g.plane_a = plane_h * 2; g.plane_b = plane_p * 2; g.M = p.dim; g.N = p.vocab; g.K = rows; g.splits = p.splits_dw;
       g.count = bound; g.first = first; g.dynamic = 2;
       if (last) { g.total = total; total.loss = nullptr; }
       if (p.splits_dw > 1) {
