@@ -404,3 +404,43 @@ def test_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(results, want)), turn
         wl = R.vocab(out, w, target)[0]
         assert R.off(loss, wl) <= SUMS
+
+
+# fp32 sizes whose products are taken in planes (all three, in one panel and in several), and just not
+PLANES = [(1100, 520, 9000, 0, 0.3), (2000, 300, 4097, 3, 0.0), (900, 136, 150001, 0, 0.1), (256, 128, 40000, 0, 0.0), (700, 1028, 3000, 0, 0.0)]
+
+
+@pytest.mark.parametrize("tokens,dim,vocab,pad,gone", PLANES)
+def test_vocab_loss_of_long_fp32_products(tokens, dim, vocab, pad, gone):
+    """Full precision whichever matrix instructions a size takes: the bounds of fp32 sums, with operands over 60 powers of two."""
+    torch, ddg, kind, t, h, w, target, weights, space = vocab_case("f32", tokens, dim, vocab, pad, gone, True)
+    gen = torch.Generator(device="cuda"); gen.manual_seed(7)
+    powers = torch.randint(-30, 31, (dim,), device="cuda", generator=gen).float()
+    h.mul_(torch.exp2(powers)); w.mul_(torch.exp2(-powers))
+    ld = dim + pad
+    op = ddg.VocabLoss(tokens, dim, vocab, kind, ld_h=ld, ld_w=ld, ld_dh=ld, ld_dw=ld)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    loss, lse, dh, dw = space(1, 1), space(1, tokens), space(tokens, dim, pad), space(vocab, dim, pad)
+    op(h, w, target, weights, loss, None, lse, dh, dw, workspace=ws)
+    wl, _, we, wdh, wdw = R.vocab(h, w, target, weights)
+    assert R.off(loss, wl) <= SUMS and R.off(lse, we) <= SUMS
+    scale = torch.exp2(powers).double()
+    assert R.off(dh.double() * scale, wdh * scale) <= GRAD["f32"] and R.off(dw.double() / scale, wdw / scale) <= GRAD["f32"]
+    assert untouched(torch, dh, pad) and untouched(torch, dw, pad)
+    again = space(vocab, dim, pad)
+    op(h, w, target, weights, dw=again, workspace=ws)
+    assert torch.equal(again, dw)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3, 7, 16, 17, 64])
+def test_loss_of_few_tokens_alone(tokens):
+    """The one-launch join of maxima and sums and the launches that more tokens take."""
+    torch, ddg, kind, t, h, w, target, weights, space = vocab_case("bf16", tokens, 72, 9001, 0, 0.3, True)
+    target[0] = 9000
+    op = ddg.VocabLoss(tokens, 72, 9001, kind)
+    ws = torch.full((op.workspace_bytes(False),), 255, device="cuda", dtype=torch.uint8)
+    for a in (weights, None):
+        loss, rows, lse = space(1, 1, dt=torch.float32), space(1, tokens, dt=torch.float32), space(1, tokens, dt=torch.float32)
+        op(h, w, target, a, loss, rows, lse, workspace=ws)
+        wl, wr, we, _, _ = R.vocab(h, w, target, a)
+        assert R.off(loss, wl) <= SUMS and R.off(rows, wr) <= SUMS and R.off(lse, we) <= SUMS
