@@ -29,6 +29,8 @@ struct ProductArgs {
   int tiles_m, tiles_n, splits;
   // epilogue 1: exp(z - m), maxima and sums, the target's logit
   void* e; long lde; float2* stat; int stats; const int* target; float* zt;   // stat: [N][stats], one of each wave's columns
+  // and where one tile holds the whole vocabulary, the rest of the way to P, if row_loss is there
+  float* row_loss; float* lse; const float* weight; int whole;
   // epilogue 2: out[map[n]][m] = scale * sum + prev
   void* out; long ldo; int out_f32; const float* prev; long ldp; const float* scale; const int* map; size_t split_stride;
   struct Total { const int* target; const float* row_loss; const float* weight; int T; float* loss; } total;   // loss null, or of one more workgroup
@@ -195,13 +197,12 @@ template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, int EP
 };
 
 template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
-__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
+__device__ __forceinline__ void product_body(const ProductArgs& a, unsigned block, unsigned char* smem) {
   typedef ProductShape<T, BM, BN, WM, WN, KB, STAGES, EPI, SPLIT> Shape;
   constexpr int NT = Shape::NT, MT = BM / WM / 32, NTL = BN / WN / 32, BK = KB / (int)sizeof(T), STEPS = KB / 32, STAGE = Shape::STAGE;
   constexpr bool INTERLEAVED = MT * NTL >= 8;
   typedef Operand<T, BM, KB, AKC, NT> OpA;
   typedef Operand<T, BN, KB, BKC, NT> OpB;
-  extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, hi = lane >> 5;
 
@@ -213,12 +214,12 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
     else K = there < K ? there : K;
   }
   // Workgroups go to the 8 XCDs round-robin: each XCD gets a run of neighbouring tiles, in bands of 8 along n, which share operands in its L2
-  const int tiles = a.tiles_m * a.tiles_n, total = tiles * a.splits, xcd = blockIdx.x & 7, q8 = total >> 3, r8 = total & 7;
-  if (EPI != EXP && blockIdx.x == (unsigned)total) {
+  const int tiles = a.tiles_m * a.tiles_n, total = tiles * a.splits, xcd = block & 7, q8 = total >> 3, r8 = total & 7;
+  if (EPI != EXP && block == (unsigned)total) {
     total_loss<NT>(a.total, smem);
     return;
   }
-  int id = q8 * xcd + (xcd < r8 ? xcd : r8) + (blockIdx.x >> 3);
+  int id = q8 * xcd + (xcd < r8 ? xcd : r8) + (block >> 3);
   const int split = id / tiles;
   id -= split * tiles;
   const int band = id / (8 * a.tiles_m), in_band = id - band * 8 * a.tiles_m, wide = a.tiles_n - band * 8 < 8 ? a.tiles_n - band * 8 : 8;
@@ -379,13 +380,13 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
           for (int e = 0; e < 16; ++e) if (mw + 32 * i + 8 * (e / 4) + e % 4 >= a.M) acc[i][j][e] = -__builtin_inff();
       }
       const int t = aim[j] < 0 ? -1 : aim[j] - mw;
+      float zt = 0.f;
       if (t >= 0 && t < 32 * MT && (t & 4) == 0 && mw + t < a.M) {   // the target is one of this lane's rows
-        float z = 0.f;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) z = t == 32 * i + 8 * (e / 4) + e % 4 ? acc[i][j][e] : z;
-        a.zt[a.first + n] = z;
+          for (int e = 0; e < 16; ++e) zt = t == 32 * i + 8 * (e / 4) + e % 4 ? acc[i][j][e] : zt;
+        if (!a.whole) a.zt[a.first + n] = zt;
       }
       float top = -__builtin_inff();
 #pragma unroll
@@ -403,7 +404,45 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
           sum += acc[i][j][e];
         }
       sum += __shfl_xor(sum, 32);
-      if (hi == 0 && n < N) a.stat[(size_t)n * a.stats + tm * WM + wm] = make_float2(from, sum);
+      if (!a.whole) {
+        if (hi == 0 && n < N) a.stat[(size_t)n * a.stats + tm * WM + wm] = make_float2(from, sum);
+      } else {
+        // The waves of a token put their maxima and sums together: its log-sum, its loss and its row of P, as vocab_row_kernel has them
+        float2* s_stat = reinterpret_cast<float2*>(smem);              // [WM][BN]
+        float* s_zt = reinterpret_cast<float*>(s_stat + WM * BN);      // [BN]
+        const int col = wn * (BN / WN) + 32 * j + l32;
+        lds_barrier();
+        if (hi == 0) s_stat[wm * BN + col] = make_float2(top, sum);
+        if (t >= 0 && t < 32 * MT && (t & 4) == 0 && mw + t < a.M) s_zt[col] = zt;
+        lds_barrier();
+        float all = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < WM; ++i) all = fmaxf(all, s_stat[i * BN + col].x);
+        const float base = all == -__builtin_inff() ? 0.f : all;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < WM; ++i) {
+          const float2 v = s_stat[i * BN + col];
+          if (v.y != 0.f) s += v.y * __expf((v.x == -__builtin_inff() ? 0.f : v.x) - base);
+        }
+        const float lse = base + logf(s), z = aim[j] >= 0 && aim[j] < a.M ? s_zt[col] : __builtin_nanf("");
+        const int token = n < N ? (a.map ? a.map[a.first + n] : a.first + n) : 0;
+        if (wm == 0 && hi == 0 && n < N) {
+          if (a.row_loss) a.row_loss[token] = aim[j] < 0 ? 0.f : lse - z;
+          if (a.lse) a.lse[token] = aim[j] < 0 ? 0.f : lse;
+        }
+        if (a.e) {
+          const float share = n < N && a.weight ? a.weight[token] / *a.scale : 1.f, by = __expf(from - lse) * share;
+          const float own = (__expf(z - base) / s - 1.f) * share;
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int m = 32 * i + 8 * (e / 4) + e % 4;
+              acc[i][j][e] = mw + m < a.M ? (t == m ? own : acc[i][j][e] * by) : 0.f;
+            }
+        }
+      }
       if (!a.e) continue;
     }
     typedef typename Shape::Staged S;
@@ -465,6 +504,19 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)
       }
     }
   }
+}
+
+extern __shared__ __align__(1024) unsigned char product_lds[];
+
+template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
+__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
+  product_body<T, BM, BN, WM, WN, KB, STAGES, AKC, BKC, EPI, SPLIT>(a, blockIdx.x, product_lds);
+}
+// Products 2 and 3 of a small call in one launch: the first n workgroups have one, the others the other
+template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES>
+__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_pair_kernel(ProductArgs a, ProductArgs b, unsigned n) {
+  if (blockIdx.x < n) product_body<T, BM, BN, WM, WN, KB, STAGES, false, true, SUM, false>(a, blockIdx.x, product_lds);
+  else product_body<T, BM, BN, WM, WN, KB, STAGES, false, false, SUM, false>(b, blockIdx.x - n, product_lds);
 }
 
 // ---- what lies between the products --------------------------------------------------------------
@@ -711,23 +763,27 @@ __global__ __launch_bounds__(1024) void vocab_few_kernel(RowArgs a, int waves, f
   *loss = (float)(a.weight ? t : t / (n > 0 ? n : 1));
 }
 
-// dh from the parts of the vocabulary, or dw from those of the tokens, in their order
+// dh from the parts of the vocabulary, dw from those of the tokens, in their order: rows of `out`, or of those in `map`
+struct Parts { const float* part; int splits; size_t stride; int rows; const int* count; int first; const int* map; void* out; long ld; int f32; };
 template <typename T>
-__global__ __launch_bounds__(256) void vocab_join_kernel(const float* part, int splits, size_t stride, int dim, const int* count, int first, int rows,
-                                                         const float* scale, const int* map, T* to, long ld) {
-  const int r = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (c >= dim || (count && first + r >= *count)) return;
+__global__ __launch_bounds__(256) void vocab_join_kernel(Parts x, Parts y, int dim, const float* scale) {
+  const Parts& a = (int)blockIdx.y < x.rows ? x : y;
+  const int r = (int)blockIdx.y < x.rows ? blockIdx.y : blockIdx.y - x.rows, c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (c >= dim || (a.count && a.first + r >= *a.count)) return;
   const int wide = (dim + 3) & ~3;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int s = 0; s < splits; ++s) {
-    const float4 q = *reinterpret_cast<const float4*>(part + s * stride + (size_t)r * wide + c);
+  for (int s = 0; s < a.splits; ++s) {
+    const float4 q = *reinterpret_cast<const float4*>(a.part + s * a.stride + (size_t)r * wide + c);
     v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
   }
-  T* out = to + (size_t)(map ? map[first + r] : first + r) * ld + c;
-
+  const size_t at = (size_t)(a.map ? a.map[a.first + r] : a.first + r) * a.ld + c;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) if (c + e < dim) Store<T>::store1(out + e, v[e] * *scale);
+  for (int e = 0; e < 4; ++e)
+    if (c + e < dim) {
+      if (a.f32) ((float*)a.out)[at + e] = v[e] * *scale;
+      else Store<T>::store1((T*)a.out + at + e, v[e] * *scale);
+    }
 }
 
 // ---- launches ------------------------------------------------------------------------------------
@@ -763,15 +819,33 @@ hipError_t product_any(const ProductArgs& a, int kind, hipStream_t s) {
   if (kind == SMALL) return product_run<T, SMALL, AKC, BKC, EPI>(a, s);
   return product_run<T, MEDIUM, AKC, BKC, EPI>(a, s);
 }
-// results in the operands' type, or in fp32, or added to earlier ones
-template <typename T, bool AKC, bool BKC> hipError_t product_out(ProductArgs a, size_t dim, int kind, hipStream_t s) {
-  const bool sum = sizeof(T) == 4 || a.out_f32 || a.prev;
+// how an epilogue that goes through 32 bits (SUM), or does not, stores its rows
+template <typename T> void set_out(ProductArgs& a, size_t dim, bool sum) {
   const size_t piece = sum ? 4 : 8, bytes = piece * (a.out_f32 || sizeof(T) == 4 ? 4 : 2);
   a.vec = dim % piece == 0 && (uintptr_t)a.out % bytes == 0 && a.ldo % piece == 0 && a.split_stride % piece == 0 &&
           (!a.prev || ((uintptr_t)a.prev % 16 == 0 && a.ldp % 4 == 0));
   a.out_f32 = a.out_f32 || sizeof(T) == 4;
+}
+// results in the operands' type, or in fp32, or added to earlier ones
+template <typename T, bool AKC, bool BKC> hipError_t product_out(ProductArgs a, size_t dim, int kind, hipStream_t s) {
+  const bool sum = sizeof(T) == 4 || a.out_f32 || a.prev;
+  set_out<T>(a, dim, sum);
   if constexpr (sizeof(T) == 4) return product_any<T, AKC, BKC, SUM>(a, kind, s);
   else return sum ? product_any<T, AKC, BKC, SUM>(a, kind, s) : product_any<T, AKC, BKC, OUT>(a, kind, s);
+}
+
+template <typename T> hipError_t product_pair(ProductArgs a, ProductArgs b, size_t dim, hipStream_t s) {
+  constexpr Tile t = TILES[SMALL];
+  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, SUM, false>::LDS;
+  static_assert(LDS <= 65536, "no attribute needed");
+  for (ProductArgs* q : {&a, &b}) {
+    set_out<T>(*q, dim, true);
+    q->tiles_m = (q->M + t.bm - 1) / t.bm;
+    q->tiles_n = (q->N + t.bn - 1) / t.bn;
+  }
+  const unsigned n = a.tiles_m * a.tiles_n * a.splits + (a.total.loss ? 1 : 0);
+  DDG_LAUNCH((product_pair_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages>), dim3(n + b.tiles_m * b.tiles_n * b.splits), dim3(t.wm * t.wn * 64), LDS, s, a, b, n);
+  return hipGetLastError();
 }
 
 size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
@@ -793,6 +867,7 @@ void vocab_plan(VocabPlan* p) {
       {{3.2f, 4.6f, 1, 14.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}},
       {{1.0f, 1.45f, 1, 9.f}, {0.68f, 1.0f, 2, 4.f}, {1.3f, 1.35f, 3, 4.f}, {0.28f, 0.7f, 3, 2.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}}};
   enum Sum { LOGITS, DH, DW };
+  constexpr float LAUNCH = 4.f;
   auto choose = [&](Sum sum, int tokens, int from, int to, int* kind, int* splits) {
     const long m = sum == LOGITS ? p->vocab : p->dim, n = sum == DW ? p->vocab : tokens, k = sum == LOGITS ? p->dim : sum == DH ? p->vocab : tokens;
     const long steps = ceil_div(k * (long)size, 128);
@@ -811,7 +886,8 @@ void vocab_plan(VocabPlan* p) {
           return (r.alone > crowded ? r.alone : crowded) * ceil_div(steps, q) + r.ends;
         };
         const float bytes = q * (float)m * n * 8.f;           // partial sums, written and read; up to 256 MB of them stay in the last cache
-        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? 4.f + bytes / (bytes < 2.4e8f ? 1e7f : 5e6f) : 0.f);
+        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? LAUNCH + bytes / (bytes < 2.4e8f ? 1e7f : 5e6f) : 0.f) +
+                        (sum == LOGITS && m > TILES[c].bm ? LAUNCH : 0.f);      // (the vocabulary in one tile: no pass over the rows)
         if (best < 0.f || t < best) { best = t; *kind = c; *splits = q; }
       }
     }
@@ -820,7 +896,20 @@ void vocab_plan(VocabPlan* p) {
   auto choose_all = [&](int tokens, int from, int to) {
     int one;
     float t = choose(LOGITS, tokens, from, to, &p->cfg_z, &one);
-    if (p->grads) t += choose(DH, tokens, from, to, &p->cfg_dh, &p->splits) + choose(DW, tokens, from, to, &p->cfg_dw, &p->splits_dw);
+    p->pair = false;
+    if (p->grads) {
+      const float apart = choose(DH, tokens, from, to, &p->cfg_dh, &p->splits) + choose(DW, tokens, from, to, &p->cfg_dw, &p->splits_dw);
+      int kinds[2], parts[2];
+      if (apart < 60.f && to > SMALL) {              // short sums: one launch of small tiles for both, and one for the parts of both
+        const float both = choose(DH, tokens, SMALL, SMALL + 1, kinds, parts) + choose(DW, tokens, SMALL, SMALL + 1, kinds + 1, parts + 1) - LAUNCH -
+                           (parts[0] > 1 && parts[1] > 1 ? LAUNCH : 0.f);
+        if (both < apart) {
+          p->pair = true;
+          p->cfg_dh = p->cfg_dw = SMALL; p->splits = parts[0]; p->splits_dw = parts[1];
+        }
+      }
+      t += apart;
+    }
     return t;
   };
   p->splits = p->splits_dw = 1;
@@ -841,7 +930,8 @@ void vocab_plan(VocabPlan* p) {
   p->panel = p->panels > 1 ? (int)up(ceil_div(p->tokens, p->panels), 256) : p->tokens;
   if (p->panels > 1) p->panels = ceil_div(p->tokens, p->panel);
   choose_all(p->panel, p->planes || b16 ? LARGE : MEDIUM, p->planes ? MEDIUM : TILE_KINDS);
-  if (p->panels > 1) p->splits_dw = 1;
+  if (p->panels > 1) { p->splits_dw = 1; p->pair = false; }
+  p->whole = p->vocab <= TILES[p->cfg_z].bm;
   p->stat_cols = TILES[p->cfg_z].bm / TILES[p->cfg_z].wm;
   p->stats = ceil_div(p->vocab, TILES[p->cfg_z].bm) * TILES[p->cfg_z].wm;
   p->acc = p->grads && p->panels > 1 && !p->dw_f32 && b16;
@@ -856,7 +946,8 @@ void vocab_plan(VocabPlan* p) {
   p->o_planes = p->grads && p->planes ? take((size_t)p->panel * p->ld_p * 6) : 0;
   const size_t operand = p->planes ? 6 : size;
   const size_t part = p->splits > 1 ? (size_t)p->splits * p->panel : 0, part_dw = p->splits_dw > 1 ? (size_t)p->splits_dw * p->vocab : 0;
-  p->o_part = p->grads ? take((part > part_dw ? part : part_dw) * up(p->dim, 4) * 4) : 0;
+  p->o_part = p->grads ? take(part * up(p->dim, 4) * 4) : 0;
+  p->o_part_dw = p->grads ? take(part_dw * up(p->dim, 4) * 4) : 0;
   p->o_acc = p->acc ? take((size_t)p->vocab * up(p->dim, 4) * 4) : 0;
   p->o_h = p->pack_h ? take(T * p->dim_p * operand) : 0;
   p->o_w = p->pack_w ? take((size_t)p->vocab * p->dim_p * operand) : 0;
@@ -921,8 +1012,9 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
     z.A = w; z.lda = ld_w; z.B = h + (size_t)first * ld_h * operand; z.ldb = ld_h; z.plane_a = plane_w * 2; z.plane_b = plane_h * 2; z.M = p.vocab; z.N = rows; z.K = p.dim_p; z.splits = 1;
     z.count = bound; z.first = first; z.dynamic = 1;
     z.e = p.grads ? a.ws + p.o_p : nullptr; z.lde = p.ld_p; z.stat = stat; z.stats = p.stats; z.target = p.pack_h ? kept : a.target; z.zt = zt;
+    if (p.whole) { z.whole = 1; z.row_loss = row_loss; z.lse = a.lse; z.weight = a.weight; z.scale = share; z.map = p.pack_h ? idx : nullptr; }
     TRY((product_any<T, true, true, EXP>(z, p.cfg_z, s)));
-    if (rows) {
+    if (rows && !p.whole) {
       RowArgs r{};
       r.stat = stat; r.stats = p.stats; r.stat_cols = p.stat_cols; r.zt = zt; r.target = z.target; r.idx = p.pack_h ? idx : nullptr; r.count = bound;
       r.weight = a.weight; r.share = share; r.first = first; r.rows = rows; r.V = p.vocab; r.row_loss = row_loss; r.lse = a.lse;
@@ -954,49 +1046,52 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
     if (!p.grads) continue;
     const bool last = panel + 1 == p.panels;
     const void* probs = a.ws + (p.planes ? p.o_planes : p.o_p);
-    // the parts of a sum, joined into rows `map` of `out`
-    auto join = [&](const ProductArgs& g, int n, int splits, const int* limit, const int* map, int at, auto* out, long ld) -> hipError_t {
-      for (int y = 0; y < n; y += 65535) {
-        const int some = n - y < 65535 ? n - y : 65535;
-        DDG_LAUNCH((vocab_join_kernel<std::remove_pointer_t<decltype(out)>>), dim3(ceil_div(p.dim, 1024), some), dim3(256), 0, s,
-                   (const float*)g.out + (size_t)y * g.ldo, splits, g.split_stride, p.dim, limit, at + y, some, (const float*)share, map, out, ld);
-        TRY(hipGetLastError());
-      }
-      return hipSuccess;
-    };
+    ProductArgs dh{}, dw{};
+    Parts parts{}, parts_dw{};
     if (a.dh && rows) {
-      ProductArgs g{};
-      g.A = w; g.lda = ld_w; g.B = probs; g.ldb = p.ld_p; g.plane_a = plane_w * 2; g.plane_b = plane_p * 2; g.M = p.dim; g.N = rows; g.K = p.vocab; g.splits = p.splits;
-      g.count = bound; g.first = first; g.dynamic = 1;
+      ProductArgs& g = dh;
+      g.A = w; g.lda = ld_w; g.B = probs; g.ldb = p.ld_p; g.plane_a = plane_w * 2; g.plane_b = plane_p * 2; g.M = p.dim; g.N = rows; g.K = p.vocab;
+      g.count = bound; g.first = first; g.dynamic = 1; g.splits = p.splits;
       if (last) { g.total = total; total.loss = nullptr; }
       if (p.splits > 1) {
         g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)rows * g.ldo;
+        parts = Parts{(const float*)g.out, p.splits, g.split_stride, rows, bound, first, idx, a.dh, a.ld_dh, size == 4};
       } else {
         g.out = a.dh; g.ldo = a.ld_dh; g.map = idx; g.scale = share;
       }
-      TRY((product_out<T, false, true>(g, p.dim, p.cfg_dh, s)));
-      if (p.splits > 1) TRY(join(g, rows, p.splits, bound, idx, first, (T*)a.dh, a.ld_dh));
     }
     if (a.dw) {
-      ProductArgs g{};
-      g.A = h + (size_t)first * ld_h * operand; g.lda = ld_h; g.B = probs; g.ldb = p.ld_p; g.plane_a = plane_h * 2; g.plane_b = plane_p * 2; g.M = p.dim; g.N = p.vocab; g.K = rows; g.splits = p.splits_dw;
-      g.count = bound; g.first = first; g.dynamic = 2;
+      ProductArgs& g = dw;
+      g.A = h + (size_t)first * ld_h * operand; g.lda = ld_h; g.B = probs; g.ldb = p.ld_p; g.plane_a = plane_h * 2; g.plane_b = plane_p * 2;
+      g.M = p.dim; g.N = p.vocab; g.K = rows; g.count = bound; g.first = first; g.dynamic = 2; g.splits = p.splits_dw;
       if (last) { g.total = total; total.loss = nullptr; }
-      if (p.splits_dw > 1) {
-        g.out = a.ws + p.o_part; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)p.vocab * g.ldo;
-        TRY((product_out<T, false, false>(g, p.dim, p.cfg_dw, s)));
-        if (p.dw_f32) TRY(join(g, p.vocab, p.splits_dw, nullptr, nullptr, 0, (float*)a.dw, a.ld_dw));
-        else TRY(join(g, p.vocab, p.splits_dw, nullptr, nullptr, 0, (T*)a.dw, a.ld_dw));
-        continue;
-      }
       const bool f32 = size == 4 || p.dw_f32;
-      float* sum = p.acc ? (float*)(a.ws + p.o_acc) : (float*)a.dw;
-      const long ld_sum = p.acc ? (long)up(p.dim, 4) : a.ld_dw;
-      if (panel) { g.prev = sum; g.ldp = ld_sum; }
-      g.scale = share;
-      g.out_f32 = f32 || !last;
-      g.out = !last ? (void*)sum : a.dw; g.ldo = !last ? ld_sum : a.ld_dw;
-      TRY((product_out<T, false, false>(g, p.dim, p.cfg_dw, s)));
+      if (p.splits_dw > 1) {
+        g.out = a.ws + p.o_part_dw; g.ldo = (long)up(p.dim, 4); g.out_f32 = 1; g.split_stride = (size_t)p.vocab * g.ldo;
+        parts_dw = Parts{(const float*)g.out, p.splits_dw, g.split_stride, p.vocab, nullptr, 0, nullptr, a.dw, a.ld_dw, f32};
+      } else {
+        float* sum = p.acc ? (float*)(a.ws + p.o_acc) : (float*)a.dw;
+        const long ld_sum = p.acc ? (long)up(p.dim, 4) : a.ld_dw;
+        if (panel) { g.prev = sum; g.ldp = ld_sum; }
+        g.scale = share;
+        g.out_f32 = f32 || !last;
+        g.out = !last ? (void*)sum : a.dw; g.ldo = !last ? ld_sum : a.ld_dw;
+      }
+    }
+    if (p.pair && dh.out && dw.out) {
+      TRY((product_pair<T>(dh, dw, p.dim, s)));
+    } else {
+      if (dh.out) TRY((product_out<T, false, true>(dh, p.dim, p.cfg_dh, s)));
+      if (dw.out) TRY((product_out<T, false, false>(dw, p.dim, p.cfg_dw, s)));
+    }
+    for (int y = 0; y < parts.rows + parts_dw.rows; y += 65535) {       // (a grid's second dimension)
+      Parts one = parts, two = parts_dw;
+      const int skip = y < one.rows ? y : one.rows, skip_dw = y - skip;
+      one.part += (size_t)skip * up(p.dim, 4); one.first += skip; one.rows -= skip;
+      two.part += (size_t)skip_dw * up(p.dim, 4); two.first += skip_dw; two.rows -= skip_dw;
+      const int n = one.rows + two.rows < 65535 ? one.rows + two.rows : 65535;
+      DDG_LAUNCH(vocab_join_kernel<T>, dim3(ceil_div(p.dim, 1024), n), dim3(256), 0, s, one, two, p.dim, (const float*)share);
+      TRY(hipGetLastError());
     }
   }
   if (total.loss) {
