@@ -188,23 +188,25 @@ __device__ constexpr int PLANES[6][2] = {{2, 0}, {1, 1}, {0, 2}, {1, 0}, {0, 1},
 // Epilogues: EXP (product 1), OUT (results in the operands' type), SUM (through 32 bits: added to earlier sums, or left in fp32)
 enum { EXP = 1, OUT = 2, SUM = 3 };
 
-template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, int EPI, bool SPLIT> struct ProductShape {
+template <typename T, int BM, int BN, int WM, int WN, int KW, int KB, int STAGES, int EPI, bool SPLIT> struct ProductShape {
   typedef std::conditional_t<EPI == SUM || SPLIT, float, T> Staged;
-  static constexpr int NT = WM * WN * 64, STAGE = (BM + BN) * KB;
+  static constexpr int NT = WM * WN * KW * 64, STAGE = (BM + BN) * KB;
   // the tile on its way out: 32 rows of each wave column at a time, rows 16 bytes apart in the banks
   static constexpr int PITCH = BM * (int)sizeof(Staged) + 16, LEAVING = WN * 32 * PITCH;
-  static constexpr int LDS = STAGES * STAGE > LEAVING ? STAGES * STAGE : LEAVING;
+  // and the sums of the waves along k on their way together
+  static constexpr int JOIN = KW > 1 ? KW * BM * BN * 4 : 0, MOST = LEAVING > JOIN ? LEAVING : JOIN;
+  static constexpr int LDS = STAGES * STAGE > MOST ? STAGES * STAGE : MOST;
 };
 
-template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
+template <typename T, int BM, int BN, int WM, int WN, int KW, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
 __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned block, unsigned char* smem) {
-  typedef ProductShape<T, BM, BN, WM, WN, KB, STAGES, EPI, SPLIT> Shape;
+  typedef ProductShape<T, BM, BN, WM, WN, KW, KB, STAGES, EPI, SPLIT> Shape;
   constexpr int NT = Shape::NT, MT = BM / WM / 32, NTL = BN / WN / 32, BK = KB / (int)sizeof(T), STEPS = KB / 32, STAGE = Shape::STAGE;
   constexpr bool INTERLEAVED = MT * NTL >= 8;
   typedef Operand<T, BM, KB, AKC, NT> OpA;
   typedef Operand<T, BN, KB, BKC, NT> OpB;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, hi = lane >> 5;
+  const int kw = wave / (WM * WN), wm = wave % (WM * WN) % WM, wn = wave % (WM * WN) / WM, l32 = lane & 31, hi = lane >> 5;
 
   int N = a.N, K = a.K;
   if (a.count) {
@@ -351,8 +353,10 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
       const unsigned char* at = smem + stage * STAGE;
       stage = stage == STAGES - 1 ? 0 : stage + 1;
       next = next == STAGES - 1 ? 0 : next + 1;
+      static_assert(STEPS % KW == 0, "");
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
+      for (int s0 = 0; s0 < STEPS / KW; ++s0) {
+        const int s = KW == 1 ? s0 : s0 * KW + kw;         // (a wave has its share of the k of each step)
         typename Frag<T>::t fa[MT], fb[NTL];
 #pragma unroll
         for (int i = 0; i < MT; ++i) fa[i] = ra.get(at, i, s);
@@ -363,6 +367,26 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
 #pragma unroll
           for (int j = 0; j < NTL; ++j) acc[i][j] = Frag<T>::mma(fa[i], fb[j], acc[i][j]);
       }
+    }
+  }
+
+  if constexpr (KW > 1) {      // the sums of the waves along k, in their order, in all of them: what follows they all do alike
+    static_assert(MT == 1 && NTL == 1, "");
+    float4* s_acc = reinterpret_cast<float4*>(smem);
+    constexpr int WAVES = WM * WN;
+    lds_barrier();
+#pragma unroll
+    for (int g = 0; g < 4; ++g) s_acc[(wave * 4 + g) * 64 + lane] = make_float4(acc[0][0][4 * g], acc[0][0][4 * g + 1], acc[0][0][4 * g + 2], acc[0][0][4 * g + 3]);
+    lds_barrier();
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float4 t = s_acc[(wave % WAVES * 4 + g) * 64 + lane];
+#pragma unroll
+      for (int q = 1; q < KW; ++q) {
+        const float4 u = s_acc[((q * WAVES + wave % WAVES) * 4 + g) * 64 + lane];
+        t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
+      }
+      acc[0][0][4 * g] = t.x; acc[0][0][4 * g + 1] = t.y; acc[0][0][4 * g + 2] = t.z; acc[0][0][4 * g + 3] = t.w;
     }
   }
 
@@ -446,11 +470,11 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
       if (!a.e) continue;
     }
     typedef typename Shape::Staged S;
-    constexpr int V = 16 / (int)sizeof(S), PIECES = BM / V, ROWS = WN * 32;
-    float4 prev[EPI == SUM ? ROWS * PIECES / NT : 1];
+    constexpr int V = 16 / (int)sizeof(S), PIECES = BM / V, ROWS = WN * 32, TURNS = (ROWS * PIECES + NT - 1) / NT;
+    float4 prev[EPI == SUM ? TURNS : 1];
     if (EPI == SUM && a.prev) {          // requested before the tile goes through LDS
 #pragma unroll
-      for (int q = 0; q < ROWS * PIECES / NT; ++q) {
+      for (int q = 0; q < TURNS; ++q) {
         const int r = (tid + q * NT) / PIECES, n = n0 + (r / 32) * (BN / WN) + 32 * j + r % 32, m = m0 + (tid + q * NT) % PIECES * V;
         prev[q] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (n >= N || m >= a.M) continue;
@@ -468,10 +492,10 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
                          acc[i][j][4 * g + 1] * scale, acc[i][j][4 * g + 2] * scale, acc[i][j][4 * g + 3] * scale);
     lds_barrier();
 #pragma unroll
-    for (int q = 0; q < ROWS * PIECES / NT; ++q) {
+    for (int q = 0; q < TURNS; ++q) {
       const int at = tid + q * NT, r = at / PIECES, c = at % PIECES;
       const int n = n0 + (r / 32) * (BN / WN) + 32 * j + r % 32, m = m0 + c * V;
-      if (n >= N) continue;
+      if (n >= N || (ROWS * PIECES % NT != 0 && at >= ROWS * PIECES)) continue;
       const S* from = reinterpret_cast<const S*>(smem + r * Shape::PITCH) + c * V;
       if (EPI == EXP) {
         if (m < a.lde) *reinterpret_cast<uint4*>((S*)a.e + (size_t)n * a.lde + m) = *reinterpret_cast<const uint4*>(from);
@@ -508,15 +532,15 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
 
 extern __shared__ __align__(1024) unsigned char product_lds[];
 
-template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
-__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
-  product_body<T, BM, BN, WM, WN, KB, STAGES, AKC, BKC, EPI, SPLIT>(a, blockIdx.x, product_lds);
+template <typename T, int BM, int BN, int WM, int WN, int KW, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
+__global__ __launch_bounds__(WM * WN * KW * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
+  product_body<T, BM, BN, WM, WN, KW, KB, STAGES, AKC, BKC, EPI, SPLIT>(a, blockIdx.x, product_lds);
 }
 // Products 2 and 3 of a small call in one launch: the first n workgroups have one, the others the other
 template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_pair_kernel(ProductArgs a, ProductArgs b, unsigned n) {
-  if (blockIdx.x < n) product_body<T, BM, BN, WM, WN, KB, STAGES, false, true, SUM, false>(a, blockIdx.x, product_lds);
-  else product_body<T, BM, BN, WM, WN, KB, STAGES, false, false, SUM, false>(b, blockIdx.x - n, product_lds);
+  if (blockIdx.x < n) product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, true, SUM, false>(a, blockIdx.x, product_lds);
+  else product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, false, SUM, false>(b, blockIdx.x - n, product_lds);
 }
 
 // ---- what lies between the products --------------------------------------------------------------
@@ -788,22 +812,23 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(Parts x, Parts y, int d
 
 // ---- launches ------------------------------------------------------------------------------------
 
-// Tiles of the products: rows along m (vocabulary or width) and n, waves along both, bytes of k in a stage, stages of LDS
-enum { LARGE, MEDIUM, SHORT, SMALL, HALF, FEW, TILE_KINDS };
-struct Tile { int bm, bn, wm, wn, kb, stages; };
-constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 64, 4}, {128, 128, 2, 2, 128, 2}, {128, 128, 2, 2, 128, 1}, {64, 64, 2, 2, 128, 3}, {128, 64, 4, 1, 128, 3}, {128, 32, 4, 1, 128, 4}};
+// Tiles of the products: rows along m (vocabulary or width) and n, waves along both and along k, bytes of k in a stage, stages of LDS
+enum { LARGE, MEDIUM, SHORT, SMALL, HALF, FEW, DEEP, TILE_KINDS };
+struct Tile { int bm, bn, wm, wn, kw, kb, stages; };
+constexpr Tile TILES[TILE_KINDS] = {{256, 256, 2, 4, 1, 64, 4}, {128, 128, 2, 2, 1, 128, 2}, {128, 128, 2, 2, 1, 128, 1}, {64, 64, 2, 2, 1, 128, 3},
+                                     {128, 64, 4, 1, 1, 128, 3}, {128, 32, 4, 1, 1, 128, 4}, {32, 32, 1, 1, 4, 128, 4}};
 
 template <typename T, int KIND, bool AKC, bool BKC, int EPI, bool SPLIT = false>
 hipError_t product_run(ProductArgs a, hipStream_t s) {
   constexpr Tile t = TILES[KIND];
-  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, EPI, SPLIT>::LDS;
-  const auto kernel = &product_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, AKC, BKC, EPI, SPLIT>;
+  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kw, t.kb, t.stages, EPI, SPLIT>::LDS;
+  const auto kernel = &product_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kw, t.kb, t.stages, AKC, BKC, EPI, SPLIT>;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (attr != hipSuccess) return attr;
   a.tiles_m = (a.M + t.bm - 1) / t.bm;
   a.tiles_n = (a.N + t.bn - 1) / t.bn;
   if (a.tiles_n == 0) return hipSuccess;
-  DDG_LAUNCH(kernel, dim3(a.tiles_m * a.tiles_n * a.splits + (a.total.loss ? 1 : 0)), dim3(t.wm * t.wn * 64), LDS, s, a);
+  DDG_LAUNCH(kernel, dim3(a.tiles_m * a.tiles_n * a.splits + (a.total.loss ? 1 : 0)), dim3(t.wm * t.wn * t.kw * 64), LDS, s, a);
   return hipGetLastError();
 }
 
@@ -811,6 +836,7 @@ template <typename T, bool AKC, bool BKC, int EPI>
 hipError_t product_any(const ProductArgs& a, int kind, hipStream_t s) {
   if constexpr (sizeof(T) == 4) if (kind == LARGE) return product_run<bf16_t, LARGE, AKC, BKC, EPI, true>(a, s);   // three planes an operand
   if constexpr (sizeof(T) == 2) if (kind == LARGE) return product_run<T, LARGE, AKC, BKC, EPI>(a, s);
+  if constexpr (AKC && BKC) if (kind == DEEP) return product_run<T, DEEP, AKC, BKC, EPI>(a, s);
   if constexpr (BKC) {
     if (kind == FEW) return product_run<T, FEW, AKC, BKC, EPI>(a, s);
     if (kind == HALF) return product_run<T, HALF, AKC, BKC, EPI>(a, s);
@@ -836,7 +862,7 @@ template <typename T, bool AKC, bool BKC> hipError_t product_out(ProductArgs a, 
 
 template <typename T> hipError_t product_pair(ProductArgs a, ProductArgs b, size_t dim, hipStream_t s) {
   constexpr Tile t = TILES[SMALL];
-  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, SUM, false>::LDS;
+  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kw, t.kb, t.stages, SUM, false>::LDS;
   static_assert(LDS <= 65536, "no attribute needed");
   for (ProductArgs* q : {&a, &b}) {
     set_out<T>(*q, dim, true);
@@ -864,8 +890,8 @@ void vocab_plan(VocabPlan* p) {
   // is in planes: six steps of bf16, of half as many bytes.
   struct Rate { float alone, full; int fit; float ends; };
   static const Rate rates[2][TILE_KINDS] = {
-      {{3.2f, 4.6f, 1, 14.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}},
-      {{1.0f, 1.45f, 1, 9.f}, {0.68f, 1.0f, 2, 4.f}, {1.3f, 1.35f, 3, 4.f}, {0.28f, 0.7f, 3, 2.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}}};
+      {{3.2f, 4.6f, 1, 14.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}, {0.25f, 0.6f, 5, 3.f}},
+      {{1.0f, 1.45f, 1, 9.f}, {0.68f, 1.0f, 2, 4.f}, {1.3f, 1.35f, 3, 4.f}, {0.28f, 0.7f, 3, 2.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}, {0.2f, 0.5f, 5, 3.f}}};
   enum Sum { LOGITS, DH, DW };
   constexpr float LAUNCH = 4.f;
   auto choose = [&](Sum sum, int tokens, int from, int to, int* kind, int* splits) {
@@ -874,7 +900,7 @@ void vocab_plan(VocabPlan* p) {
     float best = -1.f;
     *kind = from; *splits = 1;
     for (int c = from; c < to; ++c) {
-      if (sum == DW ? c > SMALL : c == SHORT) continue;
+      if (sum == DW ? c > SMALL : c == SHORT || (sum == DH && c == DEEP)) continue;
       const Rate r = rates[b16][c];
       const long tiles = (long)ceil_div(m, TILES[c].bm) * ceil_div(n, TILES[c].bn);
       for (int q = 1; q <= (sum == LOGITS ? 1 : 64) && (q == 1 || q * 2 <= steps); q = q < 4 ? q + 1 : q < 8 ? q + 2 : q + q / 2) {
