@@ -315,7 +315,7 @@ ddg_status ddg_pipeline_set_mail(ddg_pipeline* p, int k, const void* host_src, l
  * are of the descriptor's dtype unless the call says otherwise; any pointer and any ld work, 16-byte
  * pointers and rows of whole 16-byte pieces are faster. Outputs may not overlap anything else
  * that a call reads or writes, except where it says so. dry_run != 0: only the checks.
- * rows (tokens) may be 0. */
+ * rows (tokens) may be 0, and are at most 2^30, as is every ld. */
 
 /* Dropout: y = x * 65536/(65536-t) where the draw of (row, column) is t or more, else 0, with
  * t = round(65536 p), 0 <= p < 1 (t at most 65535). The draws are 16-bit pieces of Philox4x32-7
@@ -375,11 +375,13 @@ ddg_status ddg_join_norm_backward(const ddg_join_desc* d, uint64_t step, const v
  * row of dh are 0, and nothing in its row of h reaches dw. A target of vocab or more makes that
  * loss NaN. weights: fp32 [tokens], the a_i; NULL: the mean over the tokens with a target (0 if there are none).
  * loss: fp32 scalar; row_loss, lse: fp32 [tokens], unweighted; dh [tokens][dim], dw [vocab][dim] (dw_f32 != 0: in fp32 whatever the
- * dtype). Each of the five may be NULL. Products of bf16 operands are summed in fp32; with gradients in bf16, P is
+ * dtype). Each of the five may be NULL. Products of bf16 operands are summed in fp32, as are fp32 ones; lse and loss_i are differences and
+ * sums of fp32 numbers, so their error is a few 2^-24 of the logits. With gradients in bf16, P is
  * rounded to bf16 (exp(z - m) before the scale by exp(m - lse), and P after it). ddg_vocab_loss_workspace: bytes
- * of the workspace (256-byte aligned), with gradients (dh or dw) or without. It holds, besides a few words per token and the
- * gathered rows of h, at most 1040 MiB of P (or 256 tokens' where that is more), and the fp32 sum of dw if tokens take several turns;
- * more where h or w is not 16-byte aligned although its rows are whole pieces: the call then names the size. 0 if the descriptor is refused. */
+ * of the workspace (256-byte aligned), with gradients (dh or dw) or without. It holds, besides a few words per token and
+ * the gathered rows of h, at most 1040 MiB of exponentials and P (or 256 tokens' where that is more: the tokens take several turns, between which
+ * dw is summed in fp32), and parts of short sums. Long fp32 products run on the bf16 matrix instructions with every operand in three
+ * bf16 planes, which keeps 24 bits (values above 2^127 * 1.99 have no such planes: NaN): copies of h and w in 6 bytes an element. It is larger where h or w is not 16-byte aligned although its rows are whole pieces: the call then names the size. 0 if the descriptor is refused. */
 typedef struct {
   int tokens, dim, vocab, dtype;
   long ld_h, ld_w, ld_dh, ld_dw;

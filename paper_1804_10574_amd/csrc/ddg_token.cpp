@@ -65,14 +65,20 @@ template <int N, int S> ddg_status check_args(const Arg (&args)[N], const Pair (
 }
 constexpr Pair NONE[] = {{nullptr, nullptr}};
 
+// Row numbers plus the rows of a round of workgroups stay inside an int, and a tensor's extent in bytes inside 63 bits
+constexpr int ROWS_MAX = 1 << 30;
+constexpr long LD_MAX = 1l << 30;
+
 ddg_status check_rows(const char* what, int rows, int cols, int dtype) {
   if (dtype != DDG_F32 && dtype != DDG_BF16) return fail(DDG_ERR_INVALID_ARG, "%s: dtype must be DDG_F32 or DDG_BF16", what);
   if (rows < 0 || cols < 1) return fail(DDG_ERR_SHAPE, "%s: need rows >= 0 and columns >= 1 (%d, %d)", what, rows, cols);
+  if (rows > ROWS_MAX) return fail(DDG_ERR_SHAPE, "%s: at most %d rows (%d)", what, ROWS_MAX, rows);
   return DDG_OK;
 }
 ddg_status check_ld(const char* name, long* ld, int cols) {
   if (*ld == 0) *ld = cols;
   if (*ld < cols) return fail(DDG_ERR_SHAPE, "%s = %ld is less than a row of %d", name, *ld, cols);
+  if (*ld > LD_MAX) return fail(DDG_ERR_SHAPE, "%s = %ld is more than %ld", name, *ld, LD_MAX);
   return DDG_OK;
 }
 ddg_status check_drop(float p, uint64_t seed, uint64_t step, DropArgs* d) {

@@ -178,11 +178,10 @@ def _ptr(t) -> Optional[int]:
     """Device (or host) address of a torch tensor / numpy array / int / None."""
     if t is None:
         return None
-    if isinstance(t, int):
-        return t
-    if hasattr(t, "data_ptr"):
+    try:
         return t.data_ptr()
-    return t.ctypes.data
+    except AttributeError:
+        return t if isinstance(t, int) else t.ctypes.data
 
 
 def make_desc(K, k, batch, in_chw, blocks: Sequence[Sequence[int]], num_classes, compute, momentum,
@@ -441,6 +440,7 @@ class Pipeline:
 
 
 # ---- operators of token models: a descriptor each, tensors and workspace are the caller's --------
+# (Small calls take as long as the host needs for them: functions and descriptors are looked up once.)
 
 def _bytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size() if hasattr(t, "data_ptr") else t.nbytes
@@ -450,11 +450,13 @@ class Dropout:
     """ddg_dropout on [rows][cols]: the same call on the error gradient is its backward pass."""
 
     def __init__(self, rows, cols, dtype, p, seed=0, ld_x=0, ld_y=0, stream=None, dry_run=False):
-        self._lib = load_library()
         self.desc = DropoutDesc(rows, cols, dtype, p, seed, ld_x, ld_y, stream, 1 if dry_run else 0)
+        self._d, self._call = C.byref(self.desc), load_library().ddg_dropout
 
     def __call__(self, x, y, step=0):
-        _check(self._lib.ddg_dropout(self.desc, step, _ptr(x), _ptr(y)))
+        status = self._call(self._d, step, _ptr(x), _ptr(y))
+        if status:
+            _check(status)
 
 
 class JoinNorm:
@@ -462,37 +464,47 @@ class JoinNorm:
 
     def __init__(self, rows, cols, dtype, eps=1e-6, p=0.0, seed=0, ld_y=0, ld_residual=0, ld_x=0, ld_out=0, group=0,
                  stream=None, dry_run=False):
-        self._lib = load_library()
         self.desc = JoinDesc(rows, cols, dtype, eps, p, seed, ld_y, ld_residual, ld_x, ld_out, group, stream,
                              1 if dry_run else 0)
+        lib = load_library()
+        self._d, self._space = C.byref(self.desc), lib.ddg_join_norm_workspace
+        self._forward, self._q8, self._backward = lib.ddg_join_norm, lib.ddg_join_norm_q8, lib.ddg_join_norm_backward
 
     def workspace_bytes(self) -> int:
         """Bytes that `backward` needs for d_gain."""
-        return int(self._lib.ddg_join_norm_workspace(self.desc))
+        return int(self._space(self._d))
 
     def forward(self, y, residual, gain, out, x_out=None, rstd=None, step=0):
-        _check(self._lib.ddg_join_norm(self.desc, step, _ptr(y), _ptr(residual), _ptr(gain), _ptr(x_out), _ptr(out), _ptr(rstd)))
+        status = self._forward(self._d, step, _ptr(y), _ptr(residual), _ptr(gain), _ptr(x_out), _ptr(out), _ptr(rstd))
+        if status:
+            _check(status)
 
     def forward_q8(self, y, residual, gain, q, scale, x_out=None, rstd=None, step=0):
-        _check(self._lib.ddg_join_norm_q8(self.desc, step, _ptr(y), _ptr(residual), _ptr(gain), _ptr(x_out), _ptr(q), _ptr(scale),
-                                          _ptr(rstd)))
+        status = self._q8(self._d, step, _ptr(y), _ptr(residual), _ptr(gain), _ptr(x_out), _ptr(q), _ptr(scale), _ptr(rstd))
+        if status:
+            _check(status)
 
     def backward(self, x, rstd, gain, d_out, d_x=None, d_residual=None, d_y=None, d_gain=None, workspace=None, step=0):
-        _check(self._lib.ddg_join_norm_backward(self.desc, step, _ptr(x), _ptr(rstd), _ptr(gain), _ptr(d_out), _ptr(d_x),
-                                                _ptr(d_residual), _ptr(d_y), _ptr(d_gain), _ptr(workspace), _bytes(workspace)))
+        status = self._backward(self._d, step, _ptr(x), _ptr(rstd), _ptr(gain), _ptr(d_out), _ptr(d_x), _ptr(d_residual), _ptr(d_y),
+                                _ptr(d_gain), _ptr(workspace), _bytes(workspace))
+        if status:
+            _check(status)
 
 
 class VocabLoss:
     """ddg_vocab_loss: softmax cross entropy over a vocabulary and its gradients, without the logits."""
 
     def __init__(self, tokens, dim, vocab, dtype, ld_h=0, ld_w=0, ld_dh=0, ld_dw=0, dw_f32=False, stream=None, dry_run=False):
-        self._lib = load_library()
         self.desc = VocabDesc(tokens, dim, vocab, dtype, ld_h, ld_w, ld_dh, ld_dw, 1 if dw_f32 else 0, stream,
                               1 if dry_run else 0)
+        lib = load_library()
+        self._d, self._call, self._space = C.byref(self.desc), lib.ddg_vocab_loss, lib.ddg_vocab_loss_workspace
 
     def workspace_bytes(self, gradients=True) -> int:
-        return int(self._lib.ddg_vocab_loss_workspace(self.desc, 1 if gradients else 0))
+        return int(self._space(self._d, 1 if gradients else 0))
 
     def __call__(self, h, w, targets, weights=None, loss=None, row_loss=None, lse=None, dh=None, dw=None, workspace=None):
-        _check(self._lib.ddg_vocab_loss(self.desc, _ptr(h), _ptr(w), _ptr(targets), _ptr(weights), _ptr(loss), _ptr(row_loss),
-                                        _ptr(lse), _ptr(dh), _ptr(dw), _ptr(workspace), _bytes(workspace)))
+        status = self._call(self._d, _ptr(h), _ptr(w), _ptr(targets), _ptr(weights), _ptr(loss), _ptr(row_loss), _ptr(lse), _ptr(dh),
+                            _ptr(dw), _ptr(workspace), _bytes(workspace))
+        if status:
+            _check(status)

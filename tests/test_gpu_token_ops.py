@@ -444,3 +444,40 @@ def test_loss_of_few_tokens_alone(tokens):
         op(h, w, target, a, loss, rows, lse, workspace=ws)
         wl, wr, we, _, _ = R.vocab(h, w, target, a)
         assert R.off(loss, wl) <= SUMS and R.off(rows, wr) <= SUMS and R.off(lse, we) <= SUMS
+
+
+# ---- far apart -----------------------------------------------------------------------------------
+
+def test_rows_beyond_32_bits():
+    """Rows 2 and 4 MiB apart in tensors of 4.6 and 9 GB: offsets that pass 2^32 bytes and 2^31 elements, in every operand."""
+    torch, ddg, kind, t, gen, mk, space = setup("bf16")
+    rows, cols, ld = 2200, 72, 1 << 20
+    far = lambda n, step: torch.empty(n * step, device="cuda", dtype=t).view(n, step)[:, :cols]  # noqa: E731
+    x, y = far(rows, ld), far(rows, 2 * ld)
+    x.copy_(mk(rows, cols))
+    ddg.Dropout(rows, cols, kind, p=0.3, seed=SEED, ld_x=ld, ld_y=2 * ld)(x, y, step=STEP)
+    assert R.off(y, R.dropout(x, 0.3, SEED, STEP)) <= ROUND["bf16"]
+    out = space(rows, cols)
+    ddg.JoinNorm(rows, cols, kind, eps=1e-5, ld_y=ld, ld_residual=2 * ld).forward(x, y, None, out)
+    assert R.off(out, R.join(x, y, None, 1e-5)[1]) <= ROUND["bf16"]
+    # as the vocabulary's rows, and their gradients'
+    tokens = 300
+    h, target = mk(tokens, cols), torch.randint(0, rows, (tokens,), device="cuda", generator=gen, dtype=torch.int32)
+    op = ddg.VocabLoss(tokens, cols, rows, kind, ld_w=ld, ld_dw=2 * ld)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    loss, dh = space(1, 1, dt=torch.float32), space(tokens, cols)
+    op(h, x, target, None, loss, dh=dh, dw=y, workspace=ws)
+    wl, _, _, wdh, wdw = R.vocab(h, x, target)
+    assert R.off(loss, wl) <= SUMS and R.off(dh, wdh) <= GRAD["bf16"] and R.off(y, wdw) <= GRAD["bf16"]
+
+
+@pytest.mark.parametrize("dtype,dim,vocab", [("bf16", 24, 900001), ("f32", 512, 160000)])
+def test_vocab_loss_in_several_panels_with_dw_in_32_bits(dtype, dim, vocab):
+    """Also in planes (fp32, 512 wide): dw is summed over the turns in place."""
+    torch, ddg, kind, t, h, w, target, weights, space = vocab_case(dtype, 900, dim, vocab, 0, 0.1, False)
+    op = ddg.VocabLoss(900, dim, vocab, kind, dw_f32=True)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    loss, dh, dw = space(1, 1, dt=torch.float32), space(900, dim), space(vocab, dim, dt=torch.float32)
+    op(h, w, target, None, loss, None, None, dh, dw, workspace=ws)
+    wl, _, _, wdh, wdw = R.vocab(h, w, target)
+    assert R.off(loss, wl) <= SUMS and R.off(dh, wdh) <= GRAD[dtype] and R.off(dw, wdw) <= GRAD[dtype]

@@ -147,3 +147,14 @@ def test_vocab_workspace_is_bounded():
     rest = [s - o for s, o in zip(size, own)]
     assert rest[0] < rest[1] < 2.1 * 2 ** 30 and rest[3] < rest[1] + 131072 * 1024 * 4 + (1 << 28)
     assert loss(tokens=4096, **dims).workspace_bytes() < 4096 * 131072 * 4
+
+
+def test_sizes_that_no_index_holds_are_refused():
+    big = (1 << 30) + 1
+    refused(SHAPE, "at most", drop(rows=big, cols=1), A, 1 << 45)
+    refused(SHAPE, "at most", join(rows=big, cols=1).forward, A, 1 << 45, None, 1 << 46)
+    refused(SHAPE, "at most", loss(tokens=big), A, B, C_, loss=E, workspace=Space(1 << 60))
+    for ld in ("ld_x", "ld_y"):
+        refused(SHAPE, ld, drop(**{ld: big}), A, 1 << 45)
+    refused(SHAPE, "ld_dw", loss(ld_dw=1 << 62), A, B, C_, loss=E, workspace=Space(1 << 60))
+    drop(rows=1 << 30, cols=1, ld_x=1 << 30, ld_y=1 << 30)(4096, 1 << 62)
