@@ -137,11 +137,14 @@ ddg_status join_forward(const ddg_join_desc* desc, uint64_t step, const void* y,
 
 // Longest row of a tensor that the products read, in bytes: offsets inside a tile of 256 rows have 31 bits
 constexpr long ROW_BYTES_MAX = (1l << 23) - 1;
+// One workgroup of 256 threads a token: a launch holds fewer than 2^32 threads
+constexpr int TOKENS_MAX = 1 << 23;
 
 ddg_status vocab_desc(const ddg_vocab_desc* in, ddg_vocab_desc* d) {
   if (!in) return fail(DDG_ERR_INVALID_ARG, "desc is null");
   *d = *in;
   CHECK(check_rows("vocab loss", d->tokens, d->dim, d->dtype));
+  if (d->tokens > TOKENS_MAX) return fail(DDG_ERR_SHAPE, "vocab loss: at most %d tokens (%d)", TOKENS_MAX, d->tokens);
   if (d->vocab < 1) return fail(DDG_ERR_SHAPE, "vocab loss: need vocab >= 1 (%d)", d->vocab);
   CHECK(check_ld("ld_h", &d->ld_h, d->dim));
   CHECK(check_ld("ld_w", &d->ld_w, d->dim));

@@ -158,3 +158,9 @@ def test_sizes_that_no_index_holds_are_refused():
         refused(SHAPE, ld, drop(**{ld: big}), A, 1 << 45)
     refused(SHAPE, "ld_dw", loss(ld_dw=1 << 62), A, B, C_, loss=E, workspace=Space(1 << 60))
     drop(rows=1 << 30, cols=1, ld_x=1 << 30, ld_y=1 << 30)(4096, 1 << 62)
+
+
+def test_more_tokens_than_a_launch_holds_are_refused():
+    refused(SHAPE, "tokens", loss(tokens=(1 << 23) + 1), A, B, C_, loss=E, workspace=Space(1 << 60))
+    assert loss(tokens=(1 << 23) + 1).workspace_bytes() == 0
+    assert loss(tokens=1 << 23).workspace_bytes() > 0
