@@ -40,7 +40,7 @@ struct ProductArgs {
   // epilogue 2: out[map[n]][m] = scale * sum + prev
   void* out; long ldo; int out_f32; const float* prev; long ldp; const float* scale; const int* map; size_t split_stride;
   struct Total { const int* target; const float* row_loss; const float* weight; int T; float* loss; } total;   // loss null, or of one more workgroup
-  int vec;                   // rows of `out` are pieces of a store: 16 bytes (OUT), 4 elements (SUM)
+  int vec;                   // rows of `out` are pieces of a store: 16 bytes (OUT), 4 elements (SUM). Otherwise pieces wherever they begin, and the row's end one by one
 };
 
 // 16 bytes a lane from memory straight to LDS, at `lds` + 16 * lane; lanes at NOWHERE write zeros. Nothing waits here: the load has no output register,
@@ -488,6 +488,7 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
         if (n >= N || m >= a.M) continue;
         const float* from = a.prev + (size_t)n * a.ldp + m;
         if (a.vec) prev[q] = *reinterpret_cast<const float4*>(from);
+        else if (m + 4 <= a.M) __builtin_memcpy(&prev[q], from, 16);
         else prev[q] = make_float4(from[0], m + 1 < a.M ? from[1] : 0.f, m + 2 < a.M ? from[2] : 0.f, m + 3 < a.M ? from[3] : 0.f);
       }
     }
@@ -514,6 +515,8 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
       if (EPI == OUT) {
         if (a.vec) {
           *reinterpret_cast<uint4*>((T*)a.out + to) = *reinterpret_cast<const uint4*>(from);
+        } else if (m + V <= a.M) {
+          __builtin_memcpy((T*)a.out + to, from, 16);
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) if (m + e < a.M) ((T*)a.out)[to + e] = reinterpret_cast<const T*>(from)[e];
@@ -525,6 +528,13 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
         if (a.vec) {
           if (a.out_f32) Store<float>::store4((float*)a.out + to, v[0], v[1], v[2], v[3]);
           else Store<T>::store4((T*)a.out + to, v[0], v[1], v[2], v[3]);
+        } else if (m + 4 <= a.M) {
+          if (a.out_f32) {
+            __builtin_memcpy((float*)a.out + to, v, 16);
+          } else {
+            const uint2 b = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
+            __builtin_memcpy((T*)a.out + to, &b, 8);
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
