@@ -554,12 +554,14 @@ template <typename T, int BM, int BN, int WM, int WN, int KW, int KB, int STAGES
 __global__ __launch_bounds__(WM * WN * KW * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
   product_body<T, BM, BN, WM, WN, KW, KB, STAGES, AKC, BKC, EPI, SPLIT>(a, blockIdx.x, product_lds);
 }
-// Products 2 and 3 of a small call in one launch : the first n workgroups have one, the others the other. (256 fp32 tokens of width 64 over 100 entries:
-// 24.9 us with a launch for each and for the rows of P, 16.8 with this and the vocabulary in one tile.)
-template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES>
-__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_pair_kernel(ProductArgs a, ProductArgs b, unsigned n) {
-  if (blockIdx.x < n) product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, true, SUM, false>(a, blockIdx.x, product_lds);
-  else product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, false, SUM, false>(b, blockIdx.x - n, product_lds);
+// Products 2 (a) and 3 (b) in one launch, where neither of them fills the chip: the first n workgroups have one of them, the one with the longer sums, the others
+// the other. (256 fp32 tokens of width 64 over 100 entries: 24.9 us with a launch for each and for the rows of P, 16.8 with this and the vocabulary in one tile.)
+template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool SPLIT>
+__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_pair_kernel(ProductArgs a, ProductArgs b, unsigned n, int b_first) {
+  const bool second = blockIdx.x >= n;
+  const unsigned block = second ? blockIdx.x - n : blockIdx.x;
+  if (second == (b_first != 0)) product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, true, SUM, SPLIT>(a, block, product_lds);
+  else product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, false, SUM, SPLIT>(b, block, product_lds);
 }
 
 // ---- what lies between the products --------------------------------------------------------------
@@ -881,18 +883,29 @@ template <typename T, bool AKC, bool BKC> hipError_t product_out(ProductArgs a, 
   else return sum ? product_any<T, AKC, BKC, SUM>(a, kind, s) : product_any<T, AKC, BKC, OUT>(a, kind, s);
 }
 
-template <typename T> hipError_t product_pair(ProductArgs a, ProductArgs b, size_t dim, hipStream_t s) {
-  constexpr Tile t = TILES[SMALL];
-  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kw, t.kb, t.stages, SUM, false>::LDS;
-  static_assert(LDS <= 65536, "no attribute needed");
+template <typename T, int KIND, bool SPLIT = false> hipError_t product_pair_run(ProductArgs a, ProductArgs b, hipStream_t s) {
+  constexpr Tile t = TILES[KIND];
+  constexpr int LDS = ProductShape<T, t.bm, t.bn, t.wm, t.wn, t.kw, t.kb, t.stages, SUM, SPLIT>::LDS;
+  const auto kernel = &product_pair_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages, SPLIT>;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  if (attr != hipSuccess) return attr;
+  unsigned n[2];
   for (ProductArgs* q : {&a, &b}) {
-    set_out<T>(*q, dim, true);
     q->tiles_m = (q->M + t.bm - 1) / t.bm;
     q->tiles_n = (q->N + t.bn - 1) / t.bn;
+    n[q == &b] = q->tiles_m * q->tiles_n * q->splits + (q->total.loss ? 1 : 0);
   }
-  const unsigned n = a.tiles_m * a.tiles_n * a.splits + (a.total.loss ? 1 : 0);
-  DDG_LAUNCH((product_pair_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kb, t.stages>), dim3(n + b.tiles_m * b.tiles_n * b.splits), dim3(t.wm * t.wn * 64), LDS, s, a, b, n);
+  const int b_first = (long)b.K * a.splits > (long)a.K * b.splits;
+  DDG_LAUNCH(kernel, dim3(n[0] + n[1]), dim3(t.wm * t.wn * 64), LDS, s, a, b, n[b_first], b_first);
   return hipGetLastError();
+}
+template <typename T> hipError_t product_pair(ProductArgs a, ProductArgs b, size_t dim, int kind, hipStream_t s) {
+  set_out<T>(a, dim, true);
+  set_out<T>(b, dim, true);
+  if constexpr (sizeof(T) == 4) if (kind == LARGE) return product_pair_run<bf16_t, LARGE, true>(a, b, s);
+  if constexpr (sizeof(T) == 2) if (kind == LARGE) return product_pair_run<T, LARGE>(a, b, s);
+  if (kind == MEDIUM) return product_pair_run<T, MEDIUM>(a, b, s);
+  return product_pair_run<T, SMALL>(a, b, s);
 }
 
 size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
@@ -911,10 +924,19 @@ void vocab_plan(VocabPlan* p) {
   // is in planes: six steps of bf16, of half as many bytes.
   struct Rate { float alone, full; int fit; float ends; };
   static const Rate rates[2][TILE_KINDS] = {
-      {{3.2f, 4.6f, 1, 14.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}, {0.25f, 0.6f, 5, 3.f}},
+      {{3.6f, 4.9f, 1, 14.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}, {0.25f, 0.6f, 5, 3.f}},
       {{1.0f, 1.45f, 1, 9.f}, {0.68f, 1.0f, 2, 4.f}, {1.3f, 1.35f, 3, 4.f}, {0.28f, 0.7f, 3, 2.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}, {0.2f, 0.5f, 5, 3.f}}};
   enum Sum { LOGITS, DH, DW };
+  auto step_time = [](const Rate& r, long groups, int here) {      // of `groups` workgroups, `here` on the fullest compute unit
+    const float crowded = r.full * here / r.fit;
+    return r.fit == 1 ? r.alone + (r.full - r.alone) * groups / 256 : r.alone > crowded ? r.alone : crowded;
+  };
   constexpr float LAUNCH = 4.f;
+  auto more = [](int q) { return q < 3 ? q + 1 : q & (q - 1) ? q / 3 * 4 : q / 2 * 3; };     // 1, 2, 3, 4, 6, 8, 12, 16 ...
+  auto part_time = [](int q, long m, long n) {       // partial sums, written and read; up to 256 MB of them stay in the last cache
+    const float bytes = q * (float)m * n * 8.f;
+    return bytes / (bytes < 2.4e8f ? 1e7f : 5e6f);
+  };
   auto choose = [&](Sum sum, int tokens, int from, int to, int* kind, int* splits) {
     const long m = sum == LOGITS ? p->vocab : p->dim, n = sum == DW ? p->vocab : tokens, k = sum == LOGITS ? p->dim : sum == DH ? p->vocab : tokens;
     const long steps = ceil_div(k * (long)size, 128);
@@ -924,16 +946,14 @@ void vocab_plan(VocabPlan* p) {
       if (sum == DW ? c > SMALL : c == SHORT || (sum == DH && c == DEEP)) continue;
       const Rate r = rates[b16][c];
       const long tiles = (long)ceil_div(m, TILES[c].bm) * ceil_div(n, TILES[c].bn);
-      for (int q = 1; q <= (sum == LOGITS ? 1 : 64) && (q == 1 || q * 2 <= steps); q = q < 4 ? q + 1 : q < 8 ? q + 2 : q + q / 2) {
+      for (int q = 1; q <= (sum == LOGITS ? 1 : 64) && (q == 1 || q * 2 <= steps); q = more(q)) {
         const long groups = tiles * q, a_round = 256 * r.fit, last = groups % a_round;
         auto round = [&](long g) {
           if (g == 0) return 0.f;
           const int here = ceil_div(g, 256);                  // workgroups on the fullest compute unit
-          const float crowded = r.fit == 1 ? r.full * g / 256 : r.full * here / r.fit;
-          return (r.alone > crowded ? r.alone : crowded) * ceil_div(steps, q) + r.ends;
+          return step_time(r, g, here) * ceil_div(steps, q) + r.ends;
         };
-        const float bytes = q * (float)m * n * 8.f;           // partial sums, written and read; up to 256 MB of them stay in the last cache
-        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? LAUNCH + bytes / (bytes < 2.4e8f ? 1e7f : 5e6f) : 0.f) +
+        const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? LAUNCH + part_time(q, m, n) : 0.f) +
                         (sum == LOGITS && m > TILES[c].bm ? LAUNCH : 0.f);      // (the vocabulary in one tile: no pass over the rows)
         if (best < 0.f || t < best) { best = t; *kind = c; *splits = q; }
       }
@@ -946,16 +966,42 @@ void vocab_plan(VocabPlan* p) {
     p->pair = false;
     if (p->grads) {
       const float apart = choose(DH, tokens, from, to, &p->cfg_dh, &p->splits) + choose(DW, tokens, from, to, &p->cfg_dw, &p->splits_dw);
-      int kinds[2], parts[2];
-      if (apart < 60.f && to > SMALL) {              // short sums: one launch of small tiles for both, and one for the parts of both
-        const float both = choose(DH, tokens, SMALL, SMALL + 1, kinds, parts) + choose(DW, tokens, SMALL, SMALL + 1, kinds + 1, parts + 1) - LAUNCH -
-                           (parts[0] > 1 && parts[1] > 1 ? LAUNCH : 0.f);
-        if (both < apart) {
-          p->pair = true;
-          p->cfg_dh = p->cfg_dw = SMALL; p->splits = parts[0]; p->splits_dw = parts[1];
-        }
+      // Both in one launch, in tiles of one kind: the workgroups of the longer sums begin, the others fill what they leave free (one after the other: 1021 tokens of
+      // width 776 over 10007 entries 100 us a call, together 90; 4096 of 1024 over 32768 915 and 875; fp32, 512 of 512 over 8192 136 and 127)
+      float least = apart;
+      for (int c : {LARGE, MEDIUM, SMALL}) {
+        if (c < from || c >= to) continue;
+        const Rate r = rates[b16][c];
+        const long wide = ceil_div(p->dim, TILES[c].bm), steps_h = ceil_div(p->vocab * (long)size, 128), steps_w = ceil_div(tokens * (long)size, 128);
+        const long tiles_h = wide * ceil_div(tokens, TILES[c].bn), tiles_w = wide * ceil_div(p->vocab, TILES[c].bn);
+        for (int q = 1; q <= 64 && (q == 1 || (q * 2 <= steps_h && tiles_h * q <= 512 * r.fit)); q = more(q))
+          for (int w = 1; w <= 64 && (w == 1 || (w * 2 <= steps_w && tiles_w * w <= 256 * r.fit)); w = more(w)) {
+            const long all = tiles_h * q + tiles_w * w;
+            const int here = all >= 256 * r.fit ? r.fit : ceil_div(all, 256);
+            const float step = step_time(r, all < 256 ? all : 256, here);
+            const float th = step * ceil_div(steps_h, q) + r.ends, tw = step * ceil_div(steps_w, w) + r.ends;
+            const bool dw_first = tw > th;
+            const long slots = 256 * here, n1 = dw_first ? tiles_w * w : tiles_h * q, n2 = all - n1, rest = n1 % slots;
+            const float t1 = dw_first ? tw : th, t2 = dw_first ? th : tw;
+            const long k = ceil_div(n2, slots - rest);      // rounds of the shorter ones beside the last of the longer ones; where that ends first, in its places too
+            float tail = rest && k * t2 < t1 ? t1 : k * t2;
+            if (rest && k * t2 > t1) {
+              const long behind = (long)(t1 / t2), more_places = n2 - (slots - rest) * behind;
+              const float after = t1 + ceil_div(more_places, slots) * t2, in_step = ceil_div(n2 + rest * (behind + 1), slots) * t2;
+              tail = after < in_step ? after : in_step;
+            }
+            float both = (n1 / slots) * t1 + tail - LAUNCH;
+            if (q > 1 || w > 1) both += LAUNCH;
+            if (q > 1) both += part_time(q, p->dim, tokens);
+            if (w > 1) both += part_time(w, p->dim, p->vocab);
+            if (both < least) {
+              least = both;
+              p->pair = true;
+              p->cfg_dh = p->cfg_dw = c; p->splits = q; p->splits_dw = w;
+            }
+          }
       }
-      t += apart;
+      t += least;
     }
     return t;
   };
@@ -1126,7 +1172,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
       }
     }
     if (p.pair && dh.out && dw.out) {
-      TRY((product_pair<T>(dh, dw, p.dim, s)));
+      TRY((product_pair<T>(dh, dw, p.dim, p.cfg_dh, s)));
     } else {
       if (dh.out) TRY((product_out<T, false, true>(dh, p.dim, p.cfg_dh, s)));
       if (dw.out) TRY((product_out<T, false, false>(dw, p.dim, p.cfg_dw, s)));

@@ -481,3 +481,27 @@ def test_vocab_loss_in_several_panels_with_dw_in_32_bits(dtype, dim, vocab):
     op(h, w, target, None, loss, None, None, dh, dw, workspace=ws)
     wl, _, _, wdh, wdw = R.vocab(h, w, target)
     assert R.off(loss, wl) <= SUMS and R.off(dh, wdh) <= GRAD[dtype] and R.off(dw, wdw) <= GRAD[dtype]
+
+
+# sizes at which neither product of the gradients fills the chip: one launch has both, in small, middle and large tiles, with and without parts
+TOGETHER = [(1021, 777, 10007, 0), (500, 1000, 8000, 8), (700, 130, 20000, 3), (4100, 260, 1000, 0), (300, 1100, 5001, 0), (1500, 700, 15000, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,dim,vocab,pad", TOGETHER)
+@pytest.mark.parametrize("gone,dw_f32", [(0.0, False), (0.6, True)])
+def test_vocab_gradients_together(dtype, tokens, dim, vocab, pad, gone, dw_f32):
+    torch, ddg, kind, t, h, w, target, weights, space = vocab_case(dtype, tokens, dim, vocab, pad, gone, gone > 0)
+    ld = dim + pad
+    op = ddg.VocabLoss(tokens, dim, vocab, kind, ld_h=ld, ld_w=ld, ld_dh=ld, ld_dw=ld, dw_f32=dw_f32)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    wide = torch.float32 if dw_f32 else t
+    loss, dh, dw = space(1, 1, dt=torch.float32), space(tokens, dim, pad), space(vocab, dim, pad, dt=wide)
+    op(h, w, target, weights, loss, None, None, dh, dw, workspace=ws)
+    wl, _, _, wdh, wdw = R.vocab(h, w, target, weights)
+    assert R.off(loss, wl) <= SUMS and R.off(dh, wdh) <= GRAD[dtype] and R.off(dw, wdw) <= GRAD[dtype]
+    assert untouched(torch, dh, pad) and untouched(torch, dw, pad)
+    ws.fill_(255)
+    again = [space(1, 1, dt=torch.float32), space(tokens, dim, pad), space(vocab, dim, pad, dt=wide)]
+    op(h, w, target, weights, again[0], None, None, again[1], again[2], workspace=ws)
+    assert torch.equal(loss, again[0]) and torch.equal(dh, again[1]) and torch.equal(dw, again[2])
