@@ -11,7 +11,7 @@
 // out: the others are gathered first, which costs a copy of h and saves their whole share of the products.
 // bf16, 8192 tokens of width 4096 over 131072 entries: 20.6 to 21.4 ms, 1240 to 1280 TFLOP/s (product 1 1230, 2 1450, 3 1300, the pass between 5 TB/s); the library's
 // plain product of 8192^3 reaches 1413. The matrix pipes are busy 85 % of product 2's cycles and the clock has fallen from 2.4 to 1.6 GHz: power bounds it.
-// Few tokens are bound by memory: 64 over 65536 entries of width 2048 move 805 MB in 217 us (w read twice, dw written).
+// Few tokens are bound by memory: 64 over 65536 entries of width 2048 move 805 MB in 163 us, 4.9 TB/s (w read twice, dw written).
 #include "ddg_device.h"
 #include "ddg_token.h"
 
@@ -20,6 +20,7 @@
 namespace ddg {
 namespace {
 
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // ---- the product ---------------------------------------------------------------------------------
@@ -40,6 +41,7 @@ struct ProductArgs {
   // epilogue 2: out[map[n]][m] = scale * sum + prev
   void* out; long ldo; int out_f32; const float* prev; long ldp; const float* scale; const int* map; size_t split_stride;
   struct Total { const int* target; const float* row_loss; const float* weight; int T; float* loss; } total;   // loss null, or of one more workgroup
+  int past;                  // dw, in a launch of its own: results go past the caches
   int vec;                   // rows of `out` are pieces of a store: 16 bytes (OUT), 4 elements (SUM). Otherwise pieces wherever they begin, and the row's end one by one
 };
 
@@ -51,6 +53,16 @@ __device__ __forceinline__ void to_lds(u32x4 res, unsigned voff, unsigned lds) {
 // All but the last PENDING loads of this wave have arrived and every LDS read has been answered, in all waves
 template <int PENDING> __device__ __forceinline__ void step_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
+}
+// 16 or 8 bytes to memory; past the caches: nothing else is driven out of them for these
+template <typename V> __device__ __forceinline__ void put(void* to, V v, bool past) {
+  if (past) {
+    asm volatile("" ::: "memory");       // (without these the compiler makes one ordinary store of the two)
+    __builtin_nontemporal_store(v, reinterpret_cast<V*>(to));
+    asm volatile("" ::: "memory");
+  } else {
+    *reinterpret_cast<V*>(to) = v;
+  }
 }
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ u32x4 resource(const void* p) {
@@ -206,7 +218,7 @@ template <typename T, int BM, int BN, int WM, int WN, int KW, int KB, int STAGES
 };
 
 template <typename T, int BM, int BN, int WM, int WN, int KW, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
-__device__ __forceinline__ void product_body(const ProductArgs& a, unsigned block, unsigned char* smem) {
+__device__ __forceinline__ void product_body(const ProductArgs& a, unsigned block, unsigned char* smem, bool past) {
   typedef ProductShape<T, BM, BN, WM, WN, KW, KB, STAGES, EPI, SPLIT> Shape;
   constexpr int NT = Shape::NT, MT = BM / WM / 32, NTL = BN / WN / 32, BK = KB / (int)sizeof(T), STEPS = KB / 32, STAGE = Shape::STAGE;
   constexpr bool INTERLEAVED = MT * NTL >= 8;
@@ -514,7 +526,7 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
       const size_t to = a.split_stride * split + (size_t)(a.map ? a.map[a.first + n] : n) * a.ldo + m;
       if (EPI == OUT) {
         if (a.vec) {
-          *reinterpret_cast<uint4*>((T*)a.out + to) = *reinterpret_cast<const uint4*>(from);
+          put((T*)a.out + to, *reinterpret_cast<const u32x4*>(from), past);
         } else if (m + V <= a.M) {
           __builtin_memcpy((T*)a.out + to, from, 16);
         } else {
@@ -526,8 +538,8 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
         Store<float>::load4(reinterpret_cast<const float*>(from), v);
         if (a.prev) { v[0] += prev[q].x; v[1] += prev[q].y; v[2] += prev[q].z; v[3] += prev[q].w; }
         if (a.vec) {
-          if (a.out_f32) Store<float>::store4((float*)a.out + to, v[0], v[1], v[2], v[3]);
-          else Store<T>::store4((T*)a.out + to, v[0], v[1], v[2], v[3]);
+          if (a.out_f32) put((float*)a.out + to, f32x4_t{v[0], v[1], v[2], v[3]}, past);
+          else put((T*)a.out + to, u32x2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])}, past);
         } else if (m + 4 <= a.M) {
           if (a.out_f32) {
             __builtin_memcpy((float*)a.out + to, v, 16);
@@ -552,7 +564,7 @@ extern __shared__ __align__(1024) unsigned char product_lds[];
 
 template <typename T, int BM, int BN, int WM, int WN, int KW, int KB, int STAGES, bool AKC, bool BKC, int EPI, bool SPLIT>
 __global__ __launch_bounds__(WM * WN * KW * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_kernel(ProductArgs a) {
-  product_body<T, BM, BN, WM, WN, KW, KB, STAGES, AKC, BKC, EPI, SPLIT>(a, blockIdx.x, product_lds);
+  product_body<T, BM, BN, WM, WN, KW, KB, STAGES, AKC, BKC, EPI, SPLIT>(a, blockIdx.x, product_lds, !AKC && !BKC && a.past);
 }
 // Products 2 (a) and 3 (b) in one launch, where neither of them fills the chip: the first n workgroups have one of them, the one with the longer sums, the others
 // the other. (256 fp32 tokens of width 64 over 100 entries: 24.9 us with a launch for each and for the rows of P, 16.8 with this and the vocabulary in one tile.)
@@ -560,8 +572,8 @@ template <typename T, int BM, int BN, int WM, int WN, int KB, int STAGES, bool S
 __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void product_pair_kernel(ProductArgs a, ProductArgs b, unsigned n, int b_first) {
   const bool second = blockIdx.x >= n;
   const unsigned block = second ? blockIdx.x - n : blockIdx.x;
-  if (second == (b_first != 0)) product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, true, SUM, SPLIT>(a, block, product_lds);
-  else product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, false, SUM, SPLIT>(b, block, product_lds);
+  if (second == (b_first != 0)) product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, true, SUM, SPLIT>(a, block, product_lds, false);
+  else product_body<T, BM, BN, WM, WN, 1, KB, STAGES, false, false, SUM, SPLIT>(b, block, product_lds, false);
 }
 
 // ---- what lies between the products --------------------------------------------------------------
@@ -913,6 +925,11 @@ int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
 constexpr size_t PANEL_BYTES = ((size_t)1 << 30) + ((size_t)1 << 24);    // of a panel's P: 4096 tokens of a vocabulary of 131072 in bf16, a quarter of what 8192 logits in fp32 take
 
+// A dw of a quarter of the last cache or more goes past the caches: whoever reads it finds little of it there, and w, which the next call reads, would be read while dw is
+// driven out (64 tokens over entries of width 2048, back to back: 65536 of them, 268 MB of dw, 210 us through the caches and 162 past them; 32768 90.8 and 88.5;
+// 16384 56.7 and 55.6; 1024 tokens over 65536 the same). Where both gradients share a launch it gains nothing, and the choice between the two costs 1 %.
+constexpr size_t PAST_BYTES = (size_t)1 << 26;
+
 }  // namespace
 
 void vocab_plan(VocabPlan* p) {
@@ -1168,6 +1185,7 @@ template <typename T> hipError_t vocab_run(const VocabPlan& p, const VocabArgs& 
         if (panel) { g.prev = sum; g.ldp = ld_sum; }
         g.scale = share;
         g.out_f32 = f32 || !last;
+        g.past = last && (size_t)p.vocab * p.dim * (f32 ? 4 : size) >= PAST_BYTES;
         g.out = !last ? (void*)sum : a.dw; g.ldo = !last ? ld_sum : a.ld_dw;
       }
     }

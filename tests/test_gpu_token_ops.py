@@ -505,3 +505,16 @@ def test_vocab_gradients_together(dtype, tokens, dim, vocab, pad, gone, dw_f32):
     again = [space(1, 1, dt=torch.float32), space(tokens, dim, pad), space(vocab, dim, pad, dt=wide)]
     op(h, w, target, weights, again[0], None, None, again[1], again[2], workspace=ws)
     assert torch.equal(loss, again[0]) and torch.equal(dh, again[1]) and torch.equal(dw, again[2])
+
+
+@pytest.mark.parametrize("dtype,vocab,dim,dw_f32", [("bf16", 33000, 1032, False), ("bf16", 33001, 1030, False), ("bf16", 17000, 1001, True), ("f32", 9000, 2000, False)])
+def test_vocab_large_dw(dtype, vocab, dim, dw_f32):
+    """dw of 64 MiB and more (few tokens, a launch of its own), in 16-byte pieces and not, read back by another kernel."""
+    torch, ddg, kind, t, h, w, target, weights, space = vocab_case(dtype, 40, dim, vocab, 0, 0.2, True)
+    op = ddg.VocabLoss(40, dim, vocab, kind, dw_f32=dw_f32)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    loss, dh, dw = space(1, 1, dt=torch.float32), space(40, dim), space(vocab, dim, dt=torch.float32 if dw_f32 else t)
+    for _ in range(2):
+        op(h, w, target, weights, loss, None, None, dh, dw, workspace=ws)
+    wl, _, _, wdh, wdw = R.vocab(h, w, target, weights)
+    assert R.off(loss, wl) <= SUMS and R.off(dh, wdh) <= GRAD[dtype] and R.off(dw, wdw) <= GRAD[dtype]
