@@ -43,7 +43,7 @@ struct VocabPlan {
   int cfg_z, cfg_dh, cfg_dw; // tiles of the three products
   int stat_cols, stats;      // columns that share a maximum and sum, and their number
   int splits, splits_dw;     // parts of the vocabulary that dh is summed over, of the tokens that dw is
-  bool whole, pair;          // one tile holds the vocabulary; dh and dw are one launch
+  bool whole, pair;          // one tile holds the vocabulary and leaves P as it is read (not in planes); dh and dw are one launch
   bool acc;                  // dw is summed over panels in a buffer of the workspace
   size_t o_scalar, o_row, o_zt, o_stat, o_p, o_planes, o_part, o_part_dw, o_acc, o_h, o_w, bytes;
 };

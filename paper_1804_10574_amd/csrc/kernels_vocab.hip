@@ -944,6 +944,7 @@ void vocab_plan(VocabPlan* p) {
       {{3.6f, 4.9f, 1, 14.f}, {2.0f, 4.1f, 2, 4.f}, {2.6f, 6.2f, 3, 4.f}, {0.66f, 1.65f, 3, 2.f}, {1.1f, 2.05f, 2, 3.f}, {0.66f, 1.17f, 2, 3.f}, {0.25f, 0.6f, 5, 3.f}},
       {{1.0f, 1.45f, 1, 9.f}, {0.68f, 1.0f, 2, 4.f}, {1.3f, 1.35f, 3, 4.f}, {0.28f, 0.7f, 3, 2.f}, {0.37f, 0.88f, 2, 3.f}, {0.29f, 0.65f, 2, 3.f}, {0.2f, 0.5f, 5, 3.f}}};
   enum Sum { LOGITS, DH, DW };
+  auto planes_of_p = [&](int kind) { return !b16 && kind == LARGE && p->grads; };   // P in planes: the pass over the rows writes them, for one tile too
   auto step_time = [](const Rate& r, long groups, int here) {      // of `groups` workgroups, `here` on the fullest compute unit
     const float crowded = r.full * here / r.fit;
     return r.fit == 1 ? r.alone + (r.full - r.alone) * groups / 256 : r.alone > crowded ? r.alone : crowded;
@@ -971,7 +972,7 @@ void vocab_plan(VocabPlan* p) {
           return step_time(r, g, here) * ceil_div(steps, q) + r.ends;
         };
         const float t = (groups / a_round) * round(a_round) + round(last) + (q > 1 ? LAUNCH + part_time(q, m, n) : 0.f) +
-                        (sum == LOGITS && m > TILES[c].bm ? LAUNCH : 0.f);      // (the vocabulary in one tile: no pass over the rows)
+                        (sum == LOGITS && (m > TILES[c].bm || planes_of_p(c)) ? LAUNCH : 0.f);      // (the vocabulary in one tile: no pass over the rows)
         if (best < 0.f || t < best) { best = t; *kind = c; *splits = q; }
       }
     }
@@ -1041,7 +1042,7 @@ void vocab_plan(VocabPlan* p) {
   if (p->panels > 1) p->panels = ceil_div(p->tokens, p->panel);
   choose_all(p->panel, p->planes || b16 ? LARGE : MEDIUM, p->planes ? MEDIUM : TILE_KINDS);
   if (p->panels > 1) { p->splits_dw = 1; p->pair = false; }
-  p->whole = p->vocab <= TILES[p->cfg_z].bm;
+  p->whole = p->vocab <= TILES[p->cfg_z].bm && !planes_of_p(p->cfg_z);
   p->stat_cols = TILES[p->cfg_z].bm / TILES[p->cfg_z].wm;
   p->stats = ceil_div(p->vocab, TILES[p->cfg_z].bm) * TILES[p->cfg_z].wm;
   p->acc = p->grads && p->panels > 1 && !p->dw_f32 && b16;
