@@ -372,8 +372,8 @@ ddg_status ddg_join_norm_backward(const ddg_join_desc* d, uint64_t step, const v
  *   loss_i = log(sum_j exp z_ij) - z_i,target_i,   loss = sum_i a_i loss_i,
  *   dh = P w, dw = P^T h  with  P_ij = a_i (exp(z_ij - lse_i) - [j = target_i]).
  * targets: int32 [tokens]; a negative one means that the token has none: its loss, its lse and its
- * row of dh are 0, and nothing in its row of h reaches dw. A target of vocab or more makes that
- * loss NaN. weights: fp32 [tokens], the a_i; NULL: the mean over the tokens with a target (0 if there are none).
+ * row of dh are 0, and nothing in its row of h reaches dw. A target of vocab or more makes its
+ * loss, its row of dh, the loss and dw NaN. weights: fp32 [tokens], the a_i; NULL: the mean over the tokens with a target (0 if there are none).
  * loss: fp32 scalar; row_loss, lse: fp32 [tokens], unweighted; dh [tokens][dim], dw [vocab][dim] (dw_f32 != 0: in fp32 whatever the
  * dtype). Each of the five may be NULL. Products of bf16 operands are summed in fp32, as are fp32 ones; lse and loss_i are differences and
  * sums of fp32 numbers, so their error is a few 2^-24 of the logits. With gradients in bf16, P is

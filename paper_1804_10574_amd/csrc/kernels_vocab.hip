@@ -476,7 +476,7 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
           if (a.lse) a.lse[token] = aim[j] < 0 ? 0.f : lse;
         }
         if (a.e) {
-          const float share = n < N && a.weight ? a.weight[token] / *a.scale : 1.f, by = __expf(from - lse) * share;
+          const float share = aim[j] >= a.M ? __builtin_nanf("") : n < N && a.weight ? a.weight[token] / *a.scale : 1.f, by = __expf(from - lse) * share;
           const float own = (__expf(z - base) / s - 1.f) * share;
 #pragma unroll
           for (int i = 0; i < MT; ++i)
@@ -730,7 +730,7 @@ __global__ __launch_bounds__(256) void vocab_row_kernel(RowArgs a) {
   top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   const int at = a.first + r, token = a.idx ? a.idx[at] : at, y = a.target[at];
   const bool has = y >= 0 && y < a.V;
-  const float zt = has ? a.zt[at] : __builtin_nanf("");             // a target past the vocabulary: its loss is NaN, nothing is read for it
+  const float zt = has ? a.zt[at] : __builtin_nanf("");             // a target past the vocabulary: its loss and its P are NaN, nothing is read for it
   const float from = top == -__builtin_inff() ? 0.f : top;
   float sum = 0.f;
   for (int i = tid; i < a.stats; i += 256) {
@@ -747,7 +747,7 @@ __global__ __launch_bounds__(256) void vocab_row_kernel(RowArgs a) {
     if (a.lse) a.lse[token] = y < 0 ? 0.f : lse;
   }
   if (!a.p) return;
-  const float share = a.weight ? a.weight[token] / *a.share : 1.f;
+  const float share = !has ? __builtin_nanf("") : a.weight ? a.weight[token] / *a.share : 1.f;
   T* row = (T*)a.p + (size_t)r * a.ld;
   const int lo = blockIdx.x * a.chunk, hi = lo + a.chunk < a.ld ? lo + a.chunk : (int)a.ld;
   for (int c = lo + tid * V; c < hi; c += 256 * V) {
@@ -757,7 +757,7 @@ __global__ __launch_bounds__(256) void vocab_row_kernel(RowArgs a) {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       v[e] = c + e < a.V ? v[e] * scale : 0.f;
-      if (c + e == y) v[e] = (__expf(zt - from) / sum - 1.f) * share;
+      if (c + e == y && has) v[e] = (__expf(zt - from) / sum - 1.f) * share;
     }
     if constexpr (sizeof(T) == 4) {
       if (a.planes) {
