@@ -449,7 +449,8 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
         }
       sum += __shfl_xor(sum, 32);
       if (!a.whole) {
-        if (hi == 0 && n < N) a.stat[(size_t)n * a.stats + tm * WM + wm] = make_float2(from, sum);
+        // (a sum of 0 is of -inf alone: with that as its maximum the factor exp(m - lse) of these entries is 0, whatever the log-sum. A NaN sum keeps a finite one)
+        if (hi == 0 && n < N) a.stat[(size_t)n * a.stats + tm * WM + wm] = make_float2(sum == 0.f ? top : from, sum);
       } else {
         // The waves of a token put their maxima and sums together: its log-sum, its loss and its row of P, as vocab_row_kernel has them
         float2* s_stat = reinterpret_cast<float2*>(smem);              // [WM][BN]
@@ -476,7 +477,8 @@ __device__ __forceinline__ void product_body(const ProductArgs& a, unsigned bloc
           if (a.lse) a.lse[token] = aim[j] < 0 ? 0.f : lse;
         }
         if (a.e) {
-          const float share = aim[j] >= a.M ? __builtin_nanf("") : n < N && a.weight ? a.weight[token] / *a.scale : 1.f, by = __expf(from - lse) * share;
+          const float share = aim[j] >= a.M ? __builtin_nanf("") : n < N && a.weight ? a.weight[token] / *a.scale : 1.f;
+          const float by = __expf((sum == 0.f ? top : from) - lse) * share;        // (entries that are all -inf: 0, whatever the log-sum)
           const float own = (__expf(z - base) / s - 1.f) * share;
 #pragma unroll
           for (int i = 0; i < MT; ++i)
