@@ -381,7 +381,7 @@ ddg_status ddg_join_norm_backward(const ddg_join_desc* d, uint64_t step, const v
  * of the workspace (256-byte aligned), with gradients (dh or dw) or without. It holds, besides a few words per token and
  * the gathered rows of h, at most 1040 MiB of exponentials and P (or 256 tokens' where that is more: the tokens take several turns, between which
  * dw is summed in fp32), and parts of short sums. Long fp32 products run on the bf16 matrix instructions with every operand in three
- * bf16 planes, which keeps 24 bits (values above 2^127 * 1.99 have no such planes: NaN): copies of h and w in 6 bytes an element. It
+ * bf16 planes, which keeps 24 bits (infinities have no such planes: NaN): copies of h and w in 6 bytes an element. It
  * is larger where h or w is not 16-byte aligned although its rows are whole pieces: the call then names the size. 0 if the
  * descriptor is refused. At most 2^23 tokens a call. */
 typedef struct {

@@ -625,12 +625,15 @@ __global__ __launch_bounds__(1024) void vocab_scan_kernel(const int* target, con
   *share = share_of(before, weight != nullptr, top);
 }
 
-// The planes of four fp32 values, each the rounding of what the earlier ones left
+// The planes of four fp32 values, each the rounding of what the earlier ones left; the first one's stops at the largest bf16, which the lowest and highest fp32 values would
+// round past to infinity. (Infinities and NaN leave a rest that is neither 0 nor finite: NaN.)
 __device__ __forceinline__ void split4(float4 v, uint2 (&p)[3]) {
   float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    p[i] = make_uint2(f32x2_to_bf16x2(f[0], f[1]), f32x2_to_bf16x2(f[2], f[3]));
+    constexpr float MOST = 0x1.fep127f;
+    const auto whole = [&](float x) { return i == 0 ? __builtin_amdgcn_fmed3f(x, -MOST, MOST) : x; };
+    p[i] = make_uint2(f32x2_to_bf16x2(whole(f[0]), whole(f[1])), f32x2_to_bf16x2(whole(f[2]), whole(f[3])));
     f[0] -= __uint_as_float(p[i].x << 16); f[1] -= __uint_as_float(p[i].x & 0xffff0000u);
     f[2] -= __uint_as_float(p[i].y << 16); f[3] -= __uint_as_float(p[i].y & 0xffff0000u);
   }

@@ -1,4 +1,4 @@
-"""Entries of the vocabulary that are masked through a column of w (whose h is 1), in runs longer than a tile's columns: by infinity they have
+"""Entries of the vocabulary that are masked through a column of w (whose h is 1), in runs longer than a tile's columns: by infinity or by the lowest finite value they have
 the probability 0 that they have by -30000, exactly, so everything has the same bits; and it is the definition's in 64 bits (bounds as in the other tests of this operator)."""
 import pytest
 
@@ -20,7 +20,7 @@ def masked_case(dtype, tokens, dim, vocab, level):
     f32 = lambda n: space(1, n, dt=torch.float32)  # noqa: E731
 
     def call(mask):
-        w[lo:hi, 0] = mask
+        w[lo:hi, 0] = torch.finfo(t).min if mask == "lowest" else mask
         out = f32(1), f32(tokens), f32(tokens), space(tokens, dim), space(vocab, dim)
         op(h, w, target, None, *out, workspace=ws)
         return out
@@ -48,5 +48,17 @@ def test_entries_masked_by_infinity(dtype, tokens, dim, vocab, level):
     loss, rows, lse, dh, dw = got
     assert all(torch.equal(a, b) for a, b in zip((loss, rows, lse, dh[:, 1:], dw), (finite[0], finite[1], finite[2], finite[3][:, 1:], finite[4])))
     assert bool(dh[target >= 0, 0].isnan().all())           # a probability of 0 times an entry of -infinity
+    if level == 0:
+        against_definition(dtype, h, w, target, *got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,dim,vocab", [(20, 64, 100), (200, 128, 2000), (1021, 776, 10007), (40000, 1024, 256)])      # (fp32: the last two in planes)
+@pytest.mark.parametrize("level", [0.0, -200.0])
+def test_entries_masked_by_the_lowest_value(dtype, tokens, dim, vocab, level):
+    torch, call, h, w, target = masked_case(dtype, tokens, dim, vocab, level)
+    finite = call(-30000.0)
+    got = call("lowest")
+    assert all(torch.equal(a, b) for a, b in zip(got, finite))
     if level == 0:
         against_definition(dtype, h, w, target, *got)
