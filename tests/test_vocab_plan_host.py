@@ -4,7 +4,7 @@ import random
 
 import pytest
 
-from tests.vocab_plan import DEEP, FEW, HALF, LARGE, MEDIUM, ONE_TILE, ROWS, SHORT, SMALL, vocab_plan
+from tests.vocab_plan import DEEP, FEW, HALF, KINDS, LARGE, MEDIUM, ONE_TILE, PLANES, ROWS, SHORT, SMALL, kinds, vocab_plan
 
 PANEL_BYTES = (1 << 30) + (1 << 24)
 
@@ -64,3 +64,35 @@ def test_long_products_over_one_tile_are_in_planes(tokens, dim, vocab):
     p = vocab_plan("f32", tokens, dim, vocab)
     assert p.planes and not p.whole and p.cfg_z == LARGE
     assert vocab_plan("bf16", tokens, dim, vocab).whole
+
+
+@pytest.mark.parametrize("dtype,kind,sizes", [(k[0], k[1], k[2:]) for k in KINDS])
+def test_sizes_take_the_launches_that_they_are_listed_for(dtype, kind, sizes):
+    assert all(kind in kinds(vocab_plan(dtype, *s)) for s in sizes)
+    assert sorted(s[1] % 8 == 0 for s in sizes) == [False, True]
+
+
+def test_every_kind_of_launch_is_listed():
+    """Of 100000 plans up to the sizes of a training minibatch none has launches that KINDS lacks."""
+    listed, rng = {k[:2] for k in KINDS}, random.Random(11)
+    for _ in range(50000):
+        size = [round(low * (most / low) ** rng.random()) for low, most in ((20, 20000), (16, 8192), (20, 200000))]
+        for dtype in ("f32", "bf16"):
+            p = vocab_plan(dtype, *size)
+            missing = {(dtype, k) for k in kinds(p)} - listed
+            assert not missing, (size, missing)
+
+
+@pytest.mark.parametrize("size,expected", PLANES)
+def test_sizes_of_the_planes(size, expected):
+    p = vocab_plan("f32", *size)
+    assert {k: getattr(p, k) for k in expected} == expected and p.planes == expected.get("planes", True)
+
+
+def test_sizes_of_gradients_in_one_launch():
+    """What the tests of gradients in one launch are for: all of their sizes take one, and each type all three tiles, with parts and without."""
+    from tests.test_gpu_token_ops import TOGETHER
+    for dtype in ("f32", "bf16"):
+        plans = [vocab_plan(dtype, *t[:3]) for t in TOGETHER]
+        assert all(p.pair for p in plans) and {p.cfg_dh for p in plans} >= ({LARGE, SMALL, MEDIUM})
+        assert {p.splits > 1 for p in plans} == {False, True}
