@@ -382,14 +382,15 @@ ddg_status ddg_join_norm_backward(const ddg_join_desc* d, uint64_t step, const v
  * the gathered rows of h, at most 1040 MiB of exponentials and P (or 256 tokens' where that is more: the tokens take several turns, between which
  * dw is summed in fp32), and parts of short sums. Long fp32 products run on the bf16 matrix instructions with every operand in three
  * bf16 planes, which keeps 24 bits (infinities have no such planes: NaN): copies of h and w in 6 bytes an element. It
- * is larger where h or w is not 16-byte aligned although its rows are whole pieces: the call then names the size. 0 if the
- * descriptor is refused. At most 2^23 tokens a call. */
+ * is larger where h or w is not 16-byte aligned although its rows are whole pieces: `unaligned` leaves room for that (without it such a call is refused, and
+ * names the size). 0 if the descriptor is refused. At most 2^23 tokens a call. */
 typedef struct {
   int tokens, dim, vocab, dtype;
   long ld_h, ld_w, ld_dh, ld_dw;
   int dw_f32;
   void* stream;
   int dry_run;
+  int unaligned;             /* of the workspace query: h or w may lie off 16 bytes */
 } ddg_vocab_desc;
 size_t ddg_vocab_loss_workspace(const ddg_vocab_desc* d, int gradients);
 ddg_status ddg_vocab_loss(const ddg_vocab_desc* d, const void* h, const void* w, const int32_t* targets, const float* weights,

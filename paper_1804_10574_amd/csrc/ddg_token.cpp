@@ -227,12 +227,12 @@ ddg_status ddg_join_norm_backward(const ddg_join_desc* desc, uint64_t step, cons
 size_t ddg_vocab_loss_workspace(const ddg_vocab_desc* desc, int gradients) {
   ddg_vocab_desc d;
   if (vocab_desc(desc, &d) != DDG_OK) return 0;
-  // (pointers are not known yet: room for the copies that unaligned ones take is part of it where strides or width say so)
+  // (pointers are not known yet: room for the copies that unaligned ones take is part of it where strides, width or the caller say so)
   VocabPlan p{};
   p.tokens = d.tokens; p.dim = d.dim; p.vocab = d.vocab; p.dtype = d.dtype; p.grads = gradients != 0; p.dw_f32 = d.dw_f32 != 0;
   const size_t size = dtype_size(d.dtype);
-  p.pack_h = !in_pieces(nullptr, d.ld_h, d.dim, size);
-  p.pack_w = !in_pieces(nullptr, d.ld_w, d.dim, size);
+  p.pack_h = d.unaligned || !in_pieces(nullptr, d.ld_h, d.dim, size);
+  p.pack_w = d.unaligned || !in_pieces(nullptr, d.ld_w, d.dim, size);
   vocab_plan(&p);
   return p.bytes;
 }

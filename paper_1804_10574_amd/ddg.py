@@ -53,7 +53,7 @@ class JoinDesc(C.Structure):
 class VocabDesc(C.Structure):
     _fields_ = [("tokens", C.c_int), ("dim", C.c_int), ("vocab", C.c_int), ("dtype", C.c_int), ("ld_h", C.c_long),
                 ("ld_w", C.c_long), ("ld_dh", C.c_long), ("ld_dw", C.c_long), ("dw_f32", C.c_int),
-                ("stream", C.c_void_p), ("dry_run", C.c_int)]
+                ("stream", C.c_void_p), ("dry_run", C.c_int), ("unaligned", C.c_int)]
 
 
 _lib = None
@@ -492,11 +492,13 @@ class JoinNorm:
 
 
 class VocabLoss:
-    """ddg_vocab_loss: softmax cross entropy over a vocabulary and its gradients, without the logits."""
+    """ddg_vocab_loss: softmax cross entropy over a vocabulary and its gradients, without the logits. unaligned: workspace_bytes
+    leaves room for an h or w off 16 bytes."""
 
-    def __init__(self, tokens, dim, vocab, dtype, ld_h=0, ld_w=0, ld_dh=0, ld_dw=0, dw_f32=False, stream=None, dry_run=False):
+    def __init__(self, tokens, dim, vocab, dtype, ld_h=0, ld_w=0, ld_dh=0, ld_dw=0, dw_f32=False, stream=None, dry_run=False,
+                 unaligned=False):
         self.desc = VocabDesc(tokens, dim, vocab, dtype, ld_h, ld_w, ld_dh, ld_dw, 1 if dw_f32 else 0, stream,
-                              1 if dry_run else 0)
+                              1 if dry_run else 0, 1 if unaligned else 0)
         lib = load_library()
         self._d, self._call, self._space = C.byref(self.desc), lib.ddg_vocab_loss, lib.ddg_vocab_loss_workspace
 
