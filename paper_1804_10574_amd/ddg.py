@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -491,6 +492,21 @@ class JoinNorm:
             _check(status)
 
 
+@functools.lru_cache(maxsize=None)
+def _is_int32(dtype) -> bool:
+    return str(dtype).rpartition(".")[2] == "int32"
+
+
+def _int32(t, name):
+    """Whole numbers are 64 bits in torch and numpy unless asked otherwise; addresses are the caller's word."""
+    dtype = getattr(t, "dtype", None)
+    if dtype is None:
+        return
+    whole = t.is_contiguous() if hasattr(t, "is_contiguous") else t.flags.c_contiguous
+    if not whole or not _is_int32(dtype):
+        raise DDGError(1, f"{name} must be int32, next to each other ({dtype}, strides {t.stride() if hasattr(t, 'stride') else t.strides})")
+
+
 class VocabLoss:
     """ddg_vocab_loss: softmax cross entropy over a vocabulary and its gradients, without the logits. unaligned: workspace_bytes
     leaves room for an h or w off 16 bytes."""
@@ -506,6 +522,7 @@ class VocabLoss:
         return int(self._space(self._d, 1 if gradients else 0))
 
     def __call__(self, h, w, targets, weights=None, loss=None, row_loss=None, lse=None, dh=None, dw=None, workspace=None):
+        _int32(targets, "targets")
         status = self._call(self._d, _ptr(h), _ptr(w), _ptr(targets), _ptr(weights), _ptr(loss), _ptr(row_loss), _ptr(lse), _ptr(dh),
                             _ptr(dw), _ptr(workspace), _bytes(workspace))
         if status:

@@ -24,3 +24,17 @@ def test_room_for_operands_off_16_bytes(dtype, tokens, dim, vocab, gradients):
     op(False)(A, B, C_, workspace=tight, **results)
     if tight.nbytes < room.nbytes:
         refused(INVALID, "needs a workspace of", op(False), A + 4, B + 4, C_, workspace=tight, **results)
+
+
+def test_targets_of_another_type_are_refused():
+    """torch's and numpy's whole numbers are 64 bits unless asked otherwise: read as 32 they would be other targets."""
+    import numpy as np
+    import torch
+    op = ddg.VocabLoss(8, 64, 100, ddg.DDG_BF16, dry_run=True)
+    space = Space(op.workspace_bytes(False))
+    for good in (torch.zeros(8, dtype=torch.int32), torch.zeros(2, 4, dtype=torch.int32), np.zeros(8, np.int32), C_):
+        op(A, B, good, loss=E, workspace=space)
+    for bad in (torch.zeros(8, dtype=torch.int64), torch.zeros(8), torch.zeros(8, dtype=torch.int16), np.zeros(8, np.int64), np.zeros(8, np.uint32)):
+        refused(INVALID, "targets must be int32", op, A, B, bad, loss=E, workspace=space)
+    for bad in (torch.zeros(16, dtype=torch.int32)[::2], torch.zeros(2, 5, dtype=torch.int32)[:, 1:], np.zeros(16, np.int32)[::2]):
+        refused(INVALID, "targets must be int32, next to each other", op, A, B, bad, loss=E, workspace=space)
