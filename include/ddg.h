@@ -352,7 +352,7 @@ typedef struct {
 ddg_status ddg_join_norm(const ddg_join_desc* d, uint64_t step, const void* y, const void* residual, const float* gain,
                          void* x_out, void* out, float* rstd);
 /* The same with `out` in 8 bits for products of 8-bit operands: scale = max(|out| over the group) / 448
- * (fp32 [rows][groups], at least 2^-126), q = out / scale rounded to nearest even in the e4m3
+ * (fp32 [rows][groups], at least 2^-126), q = out / scale (a quotient of 32 bits) rounded to nearest even in the e4m3
  * format (4 exponent bits, 3 of fraction, largest value 448, no infinities), [rows][cols] bytes, ld_out. */
 ddg_status ddg_join_norm_q8(const ddg_join_desc* d, uint64_t step, const void* y, const void* residual, const float* gain,
                             void* x_out, uint8_t* q, float* scale, float* rstd);
