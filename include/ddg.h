@@ -377,13 +377,20 @@ ddg_status ddg_join_norm_backward(const ddg_join_desc* d, uint64_t step, const v
  * loss: fp32 scalar; row_loss, lse: fp32 [tokens], unweighted; dh [tokens][dim], dw [vocab][dim] (dw_f32 != 0: in fp32 whatever the
  * dtype). Each of the five may be NULL. Products of bf16 operands are summed in fp32, as are fp32 ones; lse and loss_i are differences and
  * sums of fp32 numbers, so their error is a few 2^-24 of the logits. With gradients in bf16, P is
- * rounded to bf16 (exp(z - m) before the scale by exp(m - lse), and P after it). ddg_vocab_loss_workspace: bytes
- * of the workspace (256-byte aligned), with gradients (dh or dw) or without. It holds, besides a few words per token and
- * the gathered rows of h, at most 1040 MiB of exponentials and P (or 256 tokens' where that is more: the tokens take several turns, between which
- * dw is summed in fp32), and parts of short sums. Long fp32 products run on the bf16 matrix instructions with every operand in three
- * bf16 planes, which keeps 24 bits (infinities have no such planes: NaN): copies of h and w in 6 bytes an element. It
- * is larger where h or w is not 16-byte aligned although its rows are whole pieces: `unaligned` leaves room for that (without it such a call is refused, and
- * names the size). 0 if the descriptor is refused. At most 2^23 tokens a call. */
+ * rounded to bf16 whatever dw_f32 says (exp(z - m) before the scale by exp(m - lse), and P after it). Long fp32 products run on the
+ * bf16 matrix instructions with every operand in three bf16 planes, which keeps 24 bits; an infinite operand has no such planes and gives NaN
+ * there, where the products of other sizes can give an infinite loss. At most 2^23 tokens a call.
+ * ddg_vocab_loss_workspace: bytes of the workspace (256-byte aligned), with gradients (dh or dw) or without; 0 if the descriptor is refused.
+ * It holds 256 bytes and 20 a token, a maximum and sum (8 bytes) for every 32 to 128 entries of a token's row, and where the call needs them
+ *   - with gradients, exponentials and P. They, or the maxima and sums of a call without gradients, take 1040 MiB at most (or 256 tokens' where that is more):
+ *     further tokens take further turns;
+ *   - vocab x dim x 4 bytes, in which dw is summed over the turns (not where dw itself is fp32);
+ *   - parts of the sums of dh (up to 64 times the tokens of a turn x dim x 4 bytes) or dw (up to 64 times vocab x dim x 4), where that is estimated to be faster
+ *     than fewer workgroups: 1.2 GB at most of the sizes that were tried;
+ *   - copies of h (gradients, or more than 64 tokens: the tokens with a target, gathered) and of w (rows that are no whole 16-byte pieces, or
+ *     pointers off 16 bytes), in rows of whole pieces; in planes copies of both, in 6 bytes an element.
+ * The query does not know the pointers: where rows are whole pieces but h or w lies off 16 bytes, `unaligned` leaves room (without it such a
+ * call is refused, and names the size). */
 typedef struct {
   int tokens, dim, vocab, dtype;
   long ld_h, ld_w, ld_dh, ld_dw;

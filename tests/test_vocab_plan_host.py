@@ -41,7 +41,8 @@ def check(dtype, tokens, dim, vocab, grads, dw_f32):
     need += [(p.o_h, tokens * p.dim_p * (6 if p.planes else size))] if p.pack_h else []
     need += [(p.o_w, vocab * p.dim_p * (6 if p.planes else size))] if p.pack_w else []
     for (at, n), (after, _) in zip(need, need[1:] + [(p.bytes, 0)]):
-        assert at % 256 == 0 and at + n <= after, where
+        assert at % 256 == 0 and at + n <= after < at + n + 256, where
+    assert 1 <= p.splits <= 64 and 1 <= p.splits_dw <= 64 and p.stat_cols in (32, 64, 128), where
 
 
 SIZES = [1, 2, 31, 64, 65, 193, 256, 257, 1021, 4096, 10007, 40000, 65536, 131072]
