@@ -9,9 +9,9 @@
 // in 32 bits and rounded once, and the factor that all tokens share is applied to the sums in 32 bits). What is kept of the T x V values is a panel's, in the
 // operands' type, of bounded size: 6 T V D flops in all, where recomputing the logits of a piece for its gradients would take 8. Tokens without a target are left
 // out: the others are gathered first, which costs a copy of h and saves their whole share of the products.
-// bf16, 8192 tokens of width 4096 over 131072 entries: 20.6 to 21.4 ms, 1240 to 1280 TFLOP/s (product 1 1230, 2 1450, 3 1300, the pass between 5 TB/s); the library's
-// plain product of 8192^3 reaches 1413. The matrix pipes are busy 85 % of product 2's cycles and the clock has fallen from 2.4 to 1.6 GHz: power bounds it.
-// Few tokens are bound by memory: 64 over 65536 entries of width 2048 move 805 MB in 163 us, 4.9 TB/s (w read twice, dw written).
+// bf16, 8192 tokens of width 4096 over 131072 entries, 5 % of them without a target: 20.7 to 21.9 ms by the card, 1150 to 1210 TFLOP/s of the others (product 1 1140, 2 1380,
+// 3 1220, the pass between 5 TB/s); the library's plain product of 8192^3 reaches 1413. The matrix pipes are busy 85 % of product 2's cycles and the clock has fallen from 2.4 to 1.6 GHz: power bounds it.
+// Few tokens are bound by memory: 64 over 65536 entries of width 2048 move 805 MB in 172 us, 4.7 TB/s (w read twice, dw written).
 #include "ddg_device.h"
 #include "ddg_token.h"
 
