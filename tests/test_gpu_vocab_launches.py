@@ -42,3 +42,19 @@ def test_every_kind_of_launch(dtype, size, gone, weighted):
 @pytest.mark.parametrize("size", [s for s, _ in PLANES])
 def test_planes_over_60_powers_of_two(size):
     check("f32", *size, 0.3, True, powers=30)
+
+
+@pytest.mark.parametrize("dtype,tokens,dim,vocab", [("bf16", 700, 16, 1200000), ("f32", 900, 512, 160000)])
+@pytest.mark.parametrize("gone", [0.9, 1.0])
+@pytest.mark.parametrize("dw_f32", [False, True])
+def test_turns_that_no_token_is_left_for(dtype, tokens, dim, vocab, gone, dw_f32):
+    """Tokens with a target fill a part of the first turn, or none: the later ones add nothing."""
+    torch, ddg, kind, t, h, w, target, weights, space = ops.vocab_case(dtype, tokens, dim, vocab, 0, gone, False)
+    if gone == 1:
+        target.fill_(-1)
+    op = ddg.VocabLoss(tokens, dim, vocab, kind, dw_f32=dw_f32)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    loss, dh, dw = space(1, 1, dt=torch.float32), space(tokens, dim), space(vocab, dim, dt=torch.float32 if dw_f32 else t)
+    op(h, w, target, None, loss, None, None, dh, dw, workspace=ws)
+    wl, _, _, wdh, wdw = R.vocab(h, w, target)
+    assert R.off(loss, wl) <= ops.SUMS and R.off(dh, wdh) <= grad(dtype, vocab) and R.off(dw, wdw) <= grad(dtype, tokens)

@@ -4,7 +4,7 @@ import random
 
 import pytest
 
-from tests.vocab_plan import DEEP, FEW, HALF, KINDS, LARGE, MEDIUM, ONE_TILE, PLANES, ROWS, SHORT, SMALL, kinds, vocab_plan
+from tests.vocab_plan import DEEP, FEW, HALF, KINDS, LARGE, LOSS_ALONE, MEDIUM, ONE_TILE, PLANES, ROWS, SHORT, SMALL, kinds, vocab_plan
 
 PANEL_BYTES = (1 << 30) + (1 << 24)
 
@@ -88,6 +88,12 @@ def test_every_kind_of_launch_is_listed():
 def test_sizes_of_the_planes(size, expected):
     p = vocab_plan("f32", *size)
     assert {k: getattr(p, k) for k in expected} == expected and p.planes == expected.get("planes", True)
+
+
+@pytest.mark.parametrize("dtype,size,expected", LOSS_ALONE)
+def test_sizes_of_the_loss_alone(dtype, size, expected):
+    p = vocab_plan(dtype, *size, grads=False)
+    assert {k: getattr(p, k) for k in expected} == expected
 
 
 def test_sizes_of_gradients_in_one_launch():

@@ -100,6 +100,12 @@ KINDS = [
 PLANES = [((1021, 777, 10007), dict(pair=True, panels=1)), ((1200, 520, 9500), dict(pair=True, panels=1)), ((469, 408, 25189), dict(pair=False, panels=1)),
           ((900, 512, 160000), dict(pair=False, panels=2)), ((40000, 1024, 256), dict(pair=True, splits_dw=48, stats=2)), ((700, 1028, 9000), dict(planes=False))]
 
+# the loss without gradients of many tokens
+LOSS_ALONE = [("f32", (40000, 1024, 256), dict(planes=False, whole=False)), ("f32", (1500, 700, 15000), dict(planes=True, panels=1)),
+              ("f32", (5000, 24, 1200001), dict(planes=False, panels=2)), ("f32", (8000, 264, 600001), dict(planes=True, panels=2)),
+              ("bf16", (40000, 1024, 256), dict(whole=True)), ("bf16", (65536, 768, 193), dict(whole=True)), ("bf16", (5000, 24, 1200001), dict(panels=2)),
+              ("bf16", (9000, 264, 200003), dict(cfg_z=LARGE, panels=1))]
+
 
 class Plan(C.Structure):       # VocabPlan
     _fields_ = ([(n, C.c_int) for n in ("tokens", "dim", "vocab", "dtype")] + [(n, C.c_bool) for n in ("grads", "dw_f32", "pack_h", "pack_w", "planes")]
