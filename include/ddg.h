@@ -403,6 +403,95 @@ size_t ddg_vocab_loss_workspace(const ddg_vocab_desc* d, int gradients);
 ddg_status ddg_vocab_loss(const ddg_vocab_desc* d, const void* h, const void* w, const int32_t* targets, const float* weights,
                           float* loss, float* row_loss, float* lse, void* dh, void* dw, void* workspace, size_t workspace_bytes);
 
+/* Rotary positions on [rows][heads * dim]: the pairs (a, b) of the first `rot` columns of every head become
+ *   ((a cos - b sin) magnitude, (b cos + a sin) magnitude) at the angle position * theta_i, i < rot / 2,
+ * the other columns stay as they are. Pairs are columns (i, i + rot/2), or with `interleaved` (2i, 2i + 1). Frequencies:
+ *   theta_i = base^(-2i/rot), for contexts longer than trained ones
+ *   theta_i / factor (context = 0), or by parts theta_i (w + (1 - w) / factor), w = (context theta_i / 2pi - low) / (high - low) within [0,1]:
+ * those that turn `high` times or more over the trained context stay, those of `low` turns or fewer are divided.
+ * The position of a row is first + positions[row] (int32), or first + row where positions is NULL; any sign. ddg_rotary_table writes the frequencies as 64-bit
+ * fractions of a turn to HOST memory (rot / 2 of them); ddg_rotary takes them from device memory, where the caller copies them once. Angles are good
+ * to 2^-32 of a turn at every position; cosines, sines and the turned pair are fp32, rounded once. inverse != 0 turns the other way: the gradient of the same call. y may be x (same ld); then
+ * columns from `rot` on are not touched. */
+typedef struct {
+  int rows, heads, dim, dtype;   /* dim: at most 1024 */
+  int rot;                       /* even, at most dim; 0: dim */
+  int interleaved;
+  double base;                   /* > 1 */
+  double factor;                 /* >= 1; 1: as trained */
+  double context, low, high;     /* context > 0: by parts, 0 <= low < high */
+  float magnitude;               /* > 0 */
+  long ld_x, ld_y;
+  void* stream;
+  int dry_run;
+} ddg_rotary_desc;
+ddg_status ddg_rotary_table(const ddg_rotary_desc* d, uint64_t* host_table);
+ddg_status ddg_rotary(const ddg_rotary_desc* d, const void* x, const int32_t* positions, long first, const uint64_t* table, int inverse, void* y);
+
+/* Linear attention with a decay g = exp(log_decay[head]) for each head: with t and s rows of one sequence, S0 its first state and len its length
+ *   o_t = scale sum_{s<=t} g^(t-s) (q_t . k_s) v_s + scale g^(t+1) q_t S0,     state_out = sum_s g^(len-1-s) k_s v_s^T + g^len S0.
+ * q [rows][heads * dim_k], k [rows][kv_heads * dim_k], v [rows][kv_heads * dim_v], o [rows][heads * dim_v]; head h reads the keys and values of
+ * h / (heads / kv_heads). log_decay: fp32 [heads], 0 or less (-inf: a row sees itself only); a constant: no gradient. g^0 is 1.
+ * starts: int32 [sequences + 1], first rows of the sequences and the end of the last; sequences may be empty, rows before the first and behind the last are
+ * not read, and theirs of the results not written. NULL: `sequences` of equal length. What lies outside [0, rows] is taken as its bound.
+ * States: fp32 [slots][heads][dim_k][dim_v], sequence n's in slots[n] (int32; NULL: n). A slot that is negative or `slots` or more: the sequence starts from 0 and its
+ * state is not kept. The slots of a call must differ. state_in NULL: S0 = 0; state_out: NULL or state_in itself or another pool; slots that no
+ * sequence names are not written. States and sums are fp32; with bf16 operands the weighted rows that make a kept state are taken apart into three bf16 pieces (two
+ * where none is kept), the state and the products q.k as operands into two: o is rounded once. Rows go in chunks of 64: an infinity or NaN in a row of v reaches the results
+ * of its sequence from up to 31 rows before it on.
+ * At most 2^23 rows; dim_k and dim_v at most 256. */
+typedef struct {
+  int rows, sequences, heads, kv_heads, dim_k, dim_v, dtype;   /* kv_heads 0: heads */
+  int slots;                     /* states in a pool; 0: sequences */
+  float scale;
+  long ld_q, ld_k, ld_v, ld_o;   /* of the gradients too */
+  void* stream;
+  int dry_run;
+} ddg_linear_desc;
+/* Bytes of the workspace (256-byte aligned): states between the segments that few long sequences are cut into (0 where they are not), in the backward pass three times
+ * that, and where heads share keys the fp32 gradients of every head. 0 too if the descriptor is refused. */
+size_t ddg_linear_attention_workspace(const ddg_linear_desc* d, int backward);
+ddg_status ddg_linear_attention(const ddg_linear_desc* d, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* starts,
+                                const int32_t* slots, const float* state_in, void* o, float* state_out, void* workspace, size_t workspace_bytes);
+/* Backward from d_o = df/do and d_state_out = df/d(state_out) (NULL: none); dq, dk, dv, d_state_in = df/d(state_in): each may be NULL. Gradients of states lie in
+ * pools of their own, by the same slots. Gradients of keys and values that heads share are summed in fp32 in a fixed order. */
+ddg_status ddg_linear_attention_backward(const ddg_linear_desc* d, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* starts,
+                                         const int32_t* slots, const float* state_in, const void* d_o, const float* d_state_out, void* dq, void* dk, void* dv,
+                                         float* d_state_in, void* workspace, size_t workspace_bytes);
+/* One row of every sequence (`rows` of them; the descriptor's `sequences` is not read): state_out = g state_in + k v^T, o = scale q state_out. fp32 throughout. */
+ddg_status ddg_linear_attention_step(const ddg_linear_desc* d, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* slots,
+                                     const float* state_in, void* o, float* state_out);
+
+/* The end of a block and the start of the next: the norm after the block, its gate, the residual, and the norm before the next block,
+ *   u = gain_y * y * rstd_y,   x = residual_scale * residual + scale * act(gate) * u,   out = gain_x * x * rstd_x,
+ * rstd = (mean of squares + eps)^(-1/2), of y over `group` neighbouring columns (0: the row), of x over the row. gate: DDG_GATE_NONE (factor 1), _COLUMN (fp32 [cols], a
+ * learned factor of each column), or [rows][cols] as it is (_PLAIN), through 1 / (1 + exp(-gate)) (_SIGMOID), or times that (_SILU). residual NULL: 0. gain_y, gain_x:
+ * fp32 [cols], NULL: 1. x_out, out, rstd_y (fp32 [rows][cols / group], or [rows]), rstd_x (fp32 [rows]): each may be NULL. x_out may be y or residual (same
+ * ld). Sums are fp32, out comes from the unrounded x. At most 16384 columns. */
+enum { DDG_GATE_NONE = 0, DDG_GATE_COLUMN = 1, DDG_GATE_PLAIN = 2, DDG_GATE_SIGMOID = 3, DDG_GATE_SILU = 4 };
+typedef struct {
+  int rows, cols, dtype;
+  float eps;                 /* > 0 */
+  float scale, residual_scale;
+  int group;                 /* columns that share a norm of y: 0, or a power of two from 8 to 512 that divides cols */
+  int gate;                  /* DDG_GATE_* */
+  long ld_y, ld_gate, ld_residual, ld_x, ld_out;
+  void* stream;
+  int dry_run;
+} ddg_gated_join_desc;
+ddg_status ddg_gated_join(const ddg_gated_join_desc* d, const void* y, const void* gate, const void* residual, const float* gain_y, const float* gain_x,
+                          void* x_out, void* out, float* rstd_y, float* rstd_x);
+/* Backward, from y, rstd_y, gate, x and rstd_x of the forward pass, d_out = df/d(out) (NULL: none; x and rstd_x may be NULL then) and d_x = df/d(x) through x_out
+ * (NULL: none), with xhat = x rstd_x, yhat = y rstd_y:
+ *   t = d_x + rstd_x (gain_x d_out - xhat mean(gain_x d_out xhat)),  d_residual = residual_scale t,  d_u = scale act(gate) t,  d_gate = scale t u act'(gate),
+ *   d_y = rstd_y (gain_y d_u - yhat mean_group(gain_y d_u yhat)),  d_gain_y = sum_rows d_u yhat,  d_gain_x = sum_rows d_out xhat.
+ * Gradients have the strides of what they belong to (ld_out: d_out, ld_x: x and d_x); d_gate is fp32 [cols], summed over rows, for a column gate. Each result may be
+ * NULL. d_residual may be d_x, if ld_residual = ld_x. Sums over rows are taken in a fixed order and need the workspace (ddg_gated_join_workspace bytes, 16-byte aligned). */
+size_t ddg_gated_join_workspace(const ddg_gated_join_desc* d);
+ddg_status ddg_gated_join_backward(const ddg_gated_join_desc* d, const void* y, const float* rstd_y, const void* gate, const void* x, const float* rstd_x,
+                                   const float* gain_y, const float* gain_x, const void* d_out, const void* d_x, void* d_residual, void* d_y, void* d_gate,
+                                   float* d_gain_y, float* d_gain_x, void* workspace, size_t workspace_bytes);
+
 /* ---- measurement ----------------------------------------------------------------------------
  * Per-kernel-family timing with HIP events on the module's stream. While enabled, every launch
  * of a kernel family is bracketed by two events; ddg_profile_read synchronises and returns, for

@@ -1,0 +1,110 @@
+// Rows of tokens in registers: what the elementwise kernels of token models (joins, rotary positions) share.
+#pragma once
+#include "ddg_device.h"
+
+namespace ddg {
+namespace {
+
+// 8 columns of a row, as they lie in memory. VEC: 16-byte pieces on their boundaries. Otherwise pieces wherever they begin (gfx950 loads and stores
+// them there too), and the row's last columns, where fewer than 8 are left, one by one with zeros behind them.
+template <typename T, bool VEC> struct Unit {
+  static constexpr int PIECES = 8 / Store<T>::VEC;
+  typedef typename Store<T>::vec_t piece_t;
+  piece_t v[PIECES];
+  __device__ __forceinline__ void load(const T* p, int n) {
+    if (VEC) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) v[i] = reinterpret_cast<const piece_t*>(p)[i];
+    } else if (n >= 8) {
+      __builtin_memcpy(v, p, sizeof(v));
+    } else {
+      T e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : T{};
+      __builtin_memcpy(v, e, sizeof(v));
+    }
+  }
+  __device__ __forceinline__ void zero() { __builtin_memset(v, 0, sizeof(v)); }
+  __device__ __forceinline__ void get(float (&o)[8]) const {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      float t[Store<T>::VEC];
+      Store<T>::unpack_vec(v[i], t);
+#pragma unroll
+      for (int j = 0; j < Store<T>::VEC; ++j) o[i * Store<T>::VEC + j] = t[j];
+    }
+  }
+  __device__ static __forceinline__ void store(T* p, const float (&o)[8], int n) {
+    Unit q;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      float t[Store<T>::VEC];
+#pragma unroll
+      for (int j = 0; j < Store<T>::VEC; ++j) t[j] = o[i * Store<T>::VEC + j];
+      Store<T>::store_vec(reinterpret_cast<T*>(&q.v[i]), t);
+    }
+    if (VEC) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) reinterpret_cast<piece_t*>(p)[i] = q.v[i];
+    } else if (n >= 8) {
+      __builtin_memcpy(p, q.v, sizeof(q.v));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (i < n) Store<T>::store1(p + i, o[i]);
+    }
+  }
+};
+
+__device__ __forceinline__ float wave_sum(float v) {
+  v = row_sum16(v);
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+__device__ __forceinline__ float row_max16(float v) {
+  v = fmaxf(v, dpp_move<0xB1>(v));
+  v = fmaxf(v, dpp_move<0x4E>(v));
+  v = fmaxf(v, dpp_move<0x141>(v));
+  return fmaxf(v, dpp_move<0x140>(v));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = row_max16(v);
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+// Of all W waves of a row, in every lane; red: W floats of LDS, of its own for each use
+template <int W> __device__ __forceinline__ float row_sum(float v, float* red) {
+  v = wave_sum(v);
+  if (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; ++i) t += red[i];
+  return t;
+}
+template <int W> __device__ __forceinline__ float row_max(float v, float* red) {
+  v = wave_max(v);
+  if (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = red[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) t = fmaxf(t, red[i]);
+  return t;
+}
+
+// The gain of a lane's columns, in registers over all the rows that it takes; 1 where there is none
+template <int U, int TPR> __device__ __forceinline__ void load_gain(const float* gain, int lane, int cols, float (&g)[U][8]) {
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int c = (lane + i * TPR) * 8 + j;
+      g[i][j] = gain && c < cols ? gain[c] : 1.f;
+    }
+}
+
+inline bool aligned(const void* p, long ld, size_t size, size_t to) { return !p || ((uintptr_t)p % to == 0 && (size_t)ld * size % to == 0); }
+
+}  // namespace
+}  // namespace ddg

@@ -8,7 +8,7 @@
 // neighbouring columns, 16 bits each, compared with limit = round(65536 p): one block per 16-byte store, where 32-bit draws would take two
 // and make the generator the bound. The kept share is then (65536 - limit) / 65536 exactly, and that is what kept elements are divided by.
 // No mask is stored: whoever needs it again (a backward pass, the re-forward of a delayed iteration) passes the same seed and step.
-#include "ddg_device.h"
+#include "ddg_rows.h"
 #include "ddg_token.h"
 
 namespace ddg {
@@ -38,56 +38,6 @@ __device__ __forceinline__ void drop8(float (&v)[8], int row, int u, const DropA
   }
 }
 
-// 8 columns of a row, as they lie in memory. VEC: 16-byte pieces on their boundaries. Otherwise pieces wherever they begin (gfx950 loads and stores
-// them there too), and the row's last columns, where fewer than 8 are left, one by one with zeros behind them.
-template <typename T, bool VEC> struct Unit {
-  static constexpr int PIECES = 8 / Store<T>::VEC;
-  typedef typename Store<T>::vec_t piece_t;
-  piece_t v[PIECES];
-  __device__ __forceinline__ void load(const T* p, int n) {
-    if (VEC) {
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) v[i] = reinterpret_cast<const piece_t*>(p)[i];
-    } else if (n >= 8) {
-      __builtin_memcpy(v, p, sizeof(v));
-    } else {
-      T e[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : T{};
-      __builtin_memcpy(v, e, sizeof(v));
-    }
-  }
-  __device__ __forceinline__ void zero() { __builtin_memset(v, 0, sizeof(v)); }
-  __device__ __forceinline__ void get(float (&o)[8]) const {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      float t[Store<T>::VEC];
-      Store<T>::unpack_vec(v[i], t);
-#pragma unroll
-      for (int j = 0; j < Store<T>::VEC; ++j) o[i * Store<T>::VEC + j] = t[j];
-    }
-  }
-  __device__ static __forceinline__ void store(T* p, const float (&o)[8], int n) {
-    Unit q;
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      float t[Store<T>::VEC];
-#pragma unroll
-      for (int j = 0; j < Store<T>::VEC; ++j) t[j] = o[i * Store<T>::VEC + j];
-      Store<T>::store_vec(reinterpret_cast<T*>(&q.v[i]), t);
-    }
-    if (VEC) {
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) reinterpret_cast<piece_t*>(p)[i] = q.v[i];
-    } else if (n >= 8) {
-      __builtin_memcpy(p, q.v, sizeof(q.v));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) if (i < n) Store<T>::store1(p + i, o[i]);
-    }
-  }
-};
-
 // ---- dropout alone -------------------------------------------------------------------------------
 
 // A 16-byte piece (fp32: two) a thread and trip; the draws' 14 products of 32 bits cost less than its loads and stores
@@ -105,55 +55,6 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int row0, i
 }
 
 // ---- the join ------------------------------------------------------------------------------------
-
-__device__ __forceinline__ float wave_sum(float v) {
-  v = row_sum16(v);
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
-}
-__device__ __forceinline__ float row_max16(float v) {
-  v = fmaxf(v, dpp_move<0xB1>(v));
-  v = fmaxf(v, dpp_move<0x4E>(v));
-  v = fmaxf(v, dpp_move<0x141>(v));
-  return fmaxf(v, dpp_move<0x140>(v));
-}
-__device__ __forceinline__ float wave_max(float v) {
-  v = row_max16(v);
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
-}
-// Of all W waves of a row, in every lane; red: W floats of LDS, of its own for each use
-template <int W> __device__ __forceinline__ float row_sum(float v, float* red) {
-  v = wave_sum(v);
-  if (W == 1) return v;
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float t = 0.f;
-#pragma unroll
-  for (int i = 0; i < W; ++i) t += red[i];
-  return t;
-}
-template <int W> __device__ __forceinline__ float row_max(float v, float* red) {
-  v = wave_max(v);
-  if (W == 1) return v;
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float t = red[0];
-#pragma unroll
-  for (int i = 1; i < W; ++i) t = fmaxf(t, red[i]);
-  return t;
-}
-
-// The gain of a lane's columns, in registers over all the rows that it takes; 1 where there is none
-template <int U, int TPR> __device__ __forceinline__ void load_gain(const float* gain, int lane, int cols, float (&g)[U][8]) {
-#pragma unroll
-  for (int i = 0; i < U; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = (lane + i * TPR) * 8 + j;
-      g[i][j] = gain && c < cols ? gain[c] : 1.f;
-    }
-}
 
 // e4m3 of a pair, round to nearest even. Values past 448 (the rounding of v * 448 / amax can pass it by a bit) become 448. NaN stays NaN.
 __device__ __forceinline__ float clamp448(float v) { return v > 448.f ? 448.f : v < -448.f ? -448.f : v; }
@@ -369,8 +270,6 @@ __global__ __launch_bounds__(1024) void join_gain_kernel(const float* partial, i
   for (int q = 1; q < 16; ++q) t += red[q * 64 + threadIdx.x];
   d_gain[c] = t;
 }
-
-bool aligned(const void* p, long ld, size_t size, size_t to) { return !p || ((uintptr_t)p % to == 0 && (size_t)ld * size % to == 0); }
 
 template <typename T, int W, int U, bool VEC>
 hipError_t forward_run(const JoinArgs& a, hipStream_t s) {

@@ -1,0 +1,588 @@
+// Linear attention with a decay g = exp(log_decay) for each head, in chunks of 64 rows. With S_t = sum_{s<=t} g^(t-s) k_s v_s^T the definition is
+//   o_t = scale S_t^T q_t.  Backward: dq_t = scale S_t do_t,  dk_t = R_t v_t,  dv_t = R_t^T k_t,  R_t = scale sum_{s>=t} g^(s-t) q_s do_s^T (+ the gradient of the last state).
+// All four are one walk over a sequence, forwards or from its end (LinearJob): a chunk of rows x, a, b with the state S before it (K x V) gives
+//   out_r = inter g^(r+1-late) x_r S + intra sum_{j<=r} g^(r-j) (x_r . a_j) b_j,    S <- g^n S + update sum_j g^(n-1-j+late) a_j b_j^T:
+// three matrix products of 64 rows for each of S's 64-column slices, 4 K V flops a row in the end where the sum over all pairs would take T (K + V).
+// A workgroup of four waves walks over a sequence (or a segment of one) for one head and one slice; S stays in its registers in 32 bits and goes to LDS once a chunk,
+// as the operand of the next product. Where there are fewer sequences and heads than the chip holds, sequences are cut into segments: a pass that only adds up
+// each segment's own state, a short scan over the segments, and the walk, which starts each segment from the state that the scan left.
+#include "ddg_device.h"
+#include "ddg_mixing.h"
+
+namespace ddg {
+namespace {
+
+constexpr int CHUNK = 64, SLICE = 64;
+
+typedef short tr4_t __attribute__((ext_vector_type(4)));
+typedef tr4_t __attribute__((address_space(3))) * tr_ptr_t;
+
+// What the two types do differently. A fragment holds KV consecutive values of the contracted index for one row or column (Mma in ddg_device.h).
+// across(): of a tile [rows][columns] in LDS the fragment whose contracted index runs over rows: those of the 16-row tiles that an accumulator has in the same lane,
+// 16 t + 4 (lane / 16) .. + 3, for as many tiles t as it takes (bf16: two). So products P that lie in accumulators are fragments without an exchange.
+template <typename T> struct Mix;
+template <> struct Mix<bf16_t> {
+  typedef Mma<bf16_t> M;
+  static constexpr int PAD = 8, TILES = 2, PLANES = 2;
+  // in every block of 16 lanes, lane s gives the address of 4 columns of row s / 4 and gets column s of the four rows
+  __device__ static __forceinline__ M::frag_t across(const bf16_t* tile, int ld, int step, int col, int lane) {
+    const bf16_t* p = tile + (32 * step + 4 * (lane >> 4) + ((lane & 15) >> 2)) * ld + col + 4 * (lane & 3);
+    const uint2 l = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr_t)(p)));
+    const uint2 h = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr_t)(p + 16 * ld)));
+    return make_uint4(l.x, l.y, h.x, h.y);
+  }
+  // an accumulator's values as operands, the sum of two: 16 bits, so that the result is rounded once
+  __device__ static __forceinline__ void split(const f32x4_t& p, uint2& h, uint2& l) {
+    h = make_uint2(f32x2_to_bf16x2(p[0], p[1]), f32x2_to_bf16x2(p[2], p[3]));
+    l = make_uint2(f32x2_to_bf16x2(p[0] - __uint_as_float(h.x << 16), p[1] - __uint_as_float(h.x & 0xffff0000u)),
+                   f32x2_to_bf16x2(p[2] - __uint_as_float(h.y << 16), p[3] - __uint_as_float(h.y & 0xffff0000u)));
+  }
+  __device__ static __forceinline__ void pack(const f32x4_t* p, M::frag_t (&o)[2]) {
+    uint2 h[2], l[2];
+    split(p[0], h[0], l[0]);
+    split(p[1], h[1], l[1]);
+    o[0] = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
+    o[1] = make_uint4(l[0].x, l[0].y, l[1].x, l[1].y);
+  }
+};
+template <> struct Mix<float> {
+  typedef Mma<float> M;
+  static constexpr int PAD = 4, TILES = 1, PLANES = 1;
+  __device__ static __forceinline__ M::frag_t across(const float* tile, int ld, int step, int col, int lane) {
+    const float* p = tile + (16 * step + 4 * (lane >> 4)) * ld + col + (lane & 15);
+    return make_float4(p[0], p[ld], p[2 * ld], p[3 * ld]);
+  }
+  __device__ static __forceinline__ void pack(const f32x4_t* p, M::frag_t (&o)[1]) { o[0] = make_float4(p[0][0], p[0][1], p[0][2], p[0][3]); }
+};
+
+// b times the rows' weights, as N fragments whose sum it is: bf16 keeps 8 bits of the product in each, fp32 all of them
+template <int N> __device__ __forceinline__ void weigh(uint4 b, const float* w, uint4 (&o)[N]) {
+  float v[8];
+  Store<bf16_t>::unpack_vec(b, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= w[i];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    o[k] = make_uint4(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7]));
+    if (k + 1 == N) break;
+    float u[8];
+    Store<bf16_t>::unpack_vec(o[k], u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] -= u[i];
+  }
+}
+template <int N> __device__ __forceinline__ void weigh(float4 b, const float* w, float4 (&o)[N]) {
+  o[0] = make_float4(b.x * w[0], b.y * w[1], b.z * w[2], b.w * w[3]);
+}
+
+// 16 bytes of n elements (n may be 0 or less: zeros)
+template <typename T, bool VEC> __device__ __forceinline__ typename Mma<T>::frag_t piece(const T* p, int n) {
+  typedef typename Mma<T>::frag_t frag_t;
+  frag_t v = Mma<T>::zero();
+  if (VEC) {
+    if (n > 0) v = *reinterpret_cast<const frag_t*>(p);
+  } else if (n >= Mma<T>::KV) {
+    __builtin_memcpy(&v, p, sizeof(v));
+  } else if (n > 0) {
+    T e[Mma<T>::KV];
+#pragma unroll
+    for (int i = 0; i < Mma<T>::KV; ++i) e[i] = i < n ? p[i] : T{};
+    __builtin_memcpy(&v, e, sizeof(v));
+  }
+  return v;
+}
+
+// Where a workgroup is: its sequence, and the rows [first, first + rows) of it, counted in the direction of the walk
+struct Place { int sequence, start, length, first, rows, segments; bool none; };
+
+__device__ __forceinline__ int clamp_row(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
+// Segments are numbered so that nobody has to add up lengths: sequence n's are start / segment + n and on, at least one each, and the numbers between are nobody's.
+// starts is device data that the host has not seen: everything is held inside [0, rows].
+__device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shared) {
+  Place p;
+  if (!g.starts) {
+    const int length = g.rows / g.sequences, per = g.split ? (length + g.segment - 1) / g.segment : 1, each = per > 0 ? per : 1;
+    p.sequence = number / each;
+    p.start = p.sequence * length;
+    p.length = length;
+    p.first = (number - p.sequence * each) * g.segment;
+    p.segments = each;
+    p.none = p.sequence >= g.sequences;
+  } else if (!g.split) {
+    p.sequence = number;
+    p.start = clamp_row(g.starts[number], g.rows);
+    p.length = max(0, clamp_row(g.starts[number + 1], g.rows) - p.start);
+    p.first = 0;
+    p.segments = 1;
+    p.none = false;
+  } else {
+    int before = 0;
+    for (int n0 = 0; n0 < g.sequences; n0 += 256) {
+      const int n = n0 + threadIdx.x;
+      const bool is = n < g.sequences && clamp_row(g.starts[n < g.sequences ? n : 0], g.rows) / g.segment + n <= number;
+      before += __popcll(__ballot(is));
+    }
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = before;
+    __syncthreads();
+    before = shared[0] + shared[1] + shared[2] + shared[3];
+    p.sequence = before - 1;
+    p.none = before < 1;
+    const int n = max(0, p.sequence);
+    p.start = clamp_row(g.starts[n], g.rows);
+    p.length = max(0, clamp_row(g.starts[n + 1], g.rows) - p.start);
+    p.first = (int)min((long)(number - (p.start / g.segment + n)) * g.segment, (long)g.rows);
+    p.segments = max(1, (p.length + g.segment - 1) / g.segment);
+    p.none |= p.first > 0 && p.first >= p.length;
+  }
+  p.sequence = __builtin_amdgcn_readfirstlane(p.sequence);
+  p.start = __builtin_amdgcn_readfirstlane(p.start);
+  p.length = __builtin_amdgcn_readfirstlane(p.length);
+  p.first = __builtin_amdgcn_readfirstlane(p.first);
+  p.segments = __builtin_amdgcn_readfirstlane(p.segments);
+  p.rows = p.length - p.first;
+  if (g.split && p.rows > g.segment) p.rows = g.segment;
+  return p;
+}
+
+// Neighbouring numbers on one of the 8 dies, whose L2 then holds what they share: workgroups go to the dies in turn
+__device__ __forceinline__ int on_die(int id, int total) {
+  const int q = total / 8, r = total % 8, die = id & 7, i = id >> 3;
+  return die < r ? die * (q + 1) + i : r * (q + 1) + (die - r) * q + i;
+}
+
+// SUM: only the state of the segment's own rows, for the scan. PLANES: fragments a weighted b is taken apart into.
+template <typename T, int DK, int PLANES, bool VEC, bool SUM>
+__global__ __launch_bounds__(256) void walk_kernel(LinearArgs g) {
+  typedef Mma<T> M;
+  typedef Mix<T> X;
+  typedef typename M::frag_t frag_t;
+  constexpr int W = M::KV, LDA = DK + X::PAD, LDB = SLICE + X::PAD, STEPS = DK / M::KSTEP, OVER = 4 / X::TILES;
+  constexpr int SPLANES = X::PLANES;                       // of S as an operand
+  constexpr int PA = CHUNK * DK / W / 256, PB = CHUNK * SLICE / W / 256;
+  extern __shared__ __align__(16) unsigned char smem[];
+  T* const at = reinterpret_cast<T*>(smem);                // [64][LDA]
+  T* const bt = at + CHUNK * LDA;                          // [64][LDB]
+  T* const st = bt + CHUNK * LDB;                          // [SPLANES][64 columns of S][LDA]
+  __shared__ float power[CHUNK + 2];
+  __shared__ int counted[4];
+
+  const LinearJob& job = g.job[blockIdx.y];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
+  const int total = g.segments * g.heads * job.slices;
+  if ((int)blockIdx.x >= total) return;
+  const int number = on_die(blockIdx.x, total), slice = number % job.slices, head = number / job.slices % g.heads;
+  const size_t segment = (size_t)(number / job.slices / g.heads);
+  const Place place = find(g, (int)segment, counted);
+  if (place.none || (SUM && place.segments == 1)) return;
+  const int K = job.K, V = job.V, v0 = slice * SLICE;
+
+  const float lam = g.log_decay[head];
+  if (tid < CHUNK + 2) power[tid] = tid ? expf((float)tid * lam) : 1.f;
+
+  // S: this wave's 16 columns, all K rows
+  f32x4_t S[DK / 16];
+  const int col = v0 + 16 * wave + l16;
+  int slot = g.slots ? g.slots[place.sequence] : place.sequence;
+  if ((unsigned)slot >= (unsigned)g.pool) slot = -1;
+  {
+    const float* from = nullptr;
+    long rk = job.at_k, rv = job.at_v;
+    if (!SUM && place.segments > 1) {
+      from = job.pieces + (segment * g.heads + head) * K * V;
+      rk = V; rv = 1;
+    } else if (!SUM && job.state_in && slot >= 0) {
+      from = job.state_in + ((size_t)slot * g.heads + head) * K * V;
+    }
+#pragma unroll
+    for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 16 * t + 4 * l4 + e;
+        S[t][e] = from && r < K && col < V ? from[r * rk + col * rv] : 0.f;
+      }
+  }
+  __syncthreads();
+
+  // factors that every chunk shares: g^(r-j) of the pairs, g^(r+1-late) of the rows, g^(n-1-j+late) of the update of a whole chunk
+  const int row = 16 * wave + l16;
+  float pairs[4][4], weight[16];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = 16 * t + 4 * l4 + e;
+      pairs[t][e] = j <= row ? job.intra * power[row - j] : 0.f;
+      weight[4 * t + e] = job.update * power[CHUNK - 1 - j + job.late];
+    }
+  const float into = job.inter * power[row + 1 - job.late];
+
+  // the rows of the walk: row r of the sequence is at base + r * step
+  const long sx = job.back ? -job.ld_x : job.ld_x, sa = job.back ? -job.ld_a : job.ld_a, sb = job.back ? -job.ld_b : job.ld_b;
+  const size_t origin = (size_t)place.start + (job.back ? (place.length ? place.length - 1 : 0) : 0);
+  const T* const bx = (const T*)job.x + origin * job.ld_x + (size_t)(head / job.share_x) * K + place.first * sx;
+  const T* const ba = (const T*)job.a + origin * job.ld_a + (size_t)(head / job.share_a) * K + place.first * sa;
+  const T* const bb = (const T*)job.b + origin * job.ld_b + (size_t)(head / job.share_b) * V + place.first * sb + v0;
+
+  frag_t xr[STEPS], ar[PA], br[PB];
+  auto request = [&](int r0) __attribute__((always_inline)) {
+    if (!SUM) {
+      const bool in = r0 + row < place.rows;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        const int c = s * M::KSTEP + l4 * W;
+        xr[s] = piece<T, VEC>(bx + (r0 + row) * sx + c, in ? K - c : 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PA; ++i) {
+      const int p = tid + i * 256, r = p / (DK / W), c = p % (DK / W) * W;
+      ar[i] = piece<T, VEC>(ba + (r0 + r) * sa + c, r0 + r < place.rows ? K - c : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      const int p = tid + i * 256, r = p / (SLICE / W), c = p % (SLICE / W) * W;
+      br[i] = piece<T, VEC>(bb + (r0 + r) * sb + c, r0 + r < place.rows ? V - v0 - c : 0);
+    }
+  };
+
+  if (place.rows > 0) request(0);
+  for (int r0 = 0; r0 < place.rows; r0 += CHUNK) {
+    const int n = min(CHUNK, place.rows - r0);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PA; ++i) {
+      const int p = tid + i * 256, r = p / (DK / W), c = p % (DK / W) * W;
+      *reinterpret_cast<frag_t*>(at + r * LDA + c) = ar[i];
+    }
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      const int p = tid + i * 256, r = p / (SLICE / W), c = p % (SLICE / W) * W;
+      *reinterpret_cast<frag_t*>(bt + r * LDB + c) = br[i];
+    }
+    if (!SUM) {
+      T* const to = st + (16 * wave + l16) * LDA + 4 * l4;
+#pragma unroll
+      for (int t = 0; t < DK / 16; ++t) {
+        if constexpr (sizeof(T) == 2) {
+          uint2 h, l;
+          X::split(S[t], h, l);
+          *reinterpret_cast<uint2*>(to + 16 * t) = h;
+          *reinterpret_cast<uint2*>(to + SLICE * LDA + 16 * t) = l;
+        } else {
+          Store<float>::store4(reinterpret_cast<float*>(to) + 16 * t, S[t][0], S[t][1], S[t][2], S[t][3]);
+        }
+      }
+    }
+    __syncthreads();
+    frag_t x[STEPS];
+    if (!SUM) {
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) x[s] = xr[s];
+    }
+    if (r0 + CHUNK < place.rows) request(r0 + CHUNK);
+    if (!SUM) {
+      // pairs of rows: this wave's 16 rows as columns, the rows before them as rows
+      f32x4_t P[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        P[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (t > wave) continue;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) P[t] = M::mma(M::load(at + (16 * t + l16) * LDA + s * M::KSTEP + l4 * W), x[s], P[t]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) P[t][e] = 16 * t + 4 * l4 + e <= row ? P[t][e] * pairs[t][e] : 0.f;
+      }
+      frag_t pairs_of[OVER][X::PLANES];
+#pragma unroll
+      for (int s = 0; s < OVER; ++s) X::pack(P + s * X::TILES, pairs_of[s]);
+      // columns of the result, 16 at a time: from the state, then from the pairs
+#pragma unroll
+      for (int t = 0; t < SLICE / 16; ++t) {
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < SPLANES; ++p)
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s) o = M::mma(M::load(st + (p * SLICE + 16 * t + l16) * LDA + s * M::KSTEP + l4 * W), x[s], o);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= into;
+#pragma unroll
+        for (int s = 0; s < OVER; ++s) {
+          if (s * X::TILES > wave) continue;
+          const frag_t b = X::across(bt, LDB, s, 16 * t, lane);
+#pragma unroll
+          for (int p = 0; p < X::PLANES; ++p) o = M::mma(b, pairs_of[s][p], o);
+        }
+        const int c = v0 + 16 * t + 4 * l4;
+        if (job.out && row < n && c < V) {
+          const size_t r = (size_t)((long)origin + (long)(place.first + r0 + row) * (job.back ? -1 : 1)), at_out = r * job.ld_out + (size_t)head * V + c;
+          if (sizeof(T) == 2 && !job.out_f32) {
+            if (VEC) Store<bf16_t>::store4((bf16_t*)job.out + at_out, o[0], o[1], o[2], o[3]);
+            else
+#pragma unroll
+              for (int e = 0; e < 4; ++e) if (c + e < V) Store<bf16_t>::store1((bf16_t*)job.out + at_out + e, o[e]);
+          } else {
+            if (VEC) Store<float>::store4((float*)job.out + at_out, o[0], o[1], o[2], o[3]);
+            else
+#pragma unroll
+              for (int e = 0; e < 4; ++e) if (c + e < V) ((float*)job.out)[at_out + e] = o[e];
+          }
+        }
+      }
+    }
+    // the state after these rows
+    if (n < CHUNK) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = 16 * t + 4 * l4 + e;
+          weight[4 * t + e] = j < n ? job.update * power[n - 1 - j + job.late] : 0.f;
+        }
+    }
+    const float keep = power[n];
+#pragma unroll
+    for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[t][e] *= keep;
+#pragma unroll
+    for (int s = 0; s < OVER; ++s) {
+      frag_t w[PLANES];
+      weigh<PLANES>(X::across(bt, LDB, s, 16 * wave, lane), weight + 4 * X::TILES * s, w);
+#pragma unroll
+      for (int t = 0; t < DK / 16; ++t) {
+        const frag_t a = X::across(at, LDA, s, 16 * t, lane);
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) S[t] = M::mma(a, w[p], S[t]);
+      }
+    }
+  }
+
+  float* to = nullptr;
+  long rk = job.at_k, rv = job.at_v;
+  if (SUM) {
+    to = job.pieces + (segment * g.heads + head) * K * V;
+    rk = V; rv = 1;
+  } else if (place.segments == 1 && job.state_out && slot >= 0) {
+    to = job.state_out + ((size_t)slot * g.heads + head) * K * V;
+  }
+  if (!to) return;
+#pragma unroll
+  for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 16 * t + 4 * l4 + e;
+      if (r < K && col < V) to[r * rk + col * rv] = S[t][e];
+    }
+}
+
+// The states before each segment from the segments' own, in place, and the last one: a thread an element, segments in order
+__global__ __launch_bounds__(256) void scan_kernel(LinearArgs g, int blocks) {
+  const LinearJob& job = g.job[blockIdx.y];
+  const int K = job.K, V = job.V, pair = blockIdx.x / blocks, n = pair / g.heads, head = pair % g.heads;
+  int start, length, first;
+  if (g.starts) {
+    start = clamp_row(g.starts[n], g.rows);
+    length = max(0, clamp_row(g.starts[n + 1], g.rows) - start);
+    first = start / g.segment + n;
+  } else {
+    length = g.rows / g.sequences;
+    first = n * max(1, (length + g.segment - 1) / g.segment);
+  }
+  const int count = (length + g.segment - 1) / g.segment;
+  const int i = (blockIdx.x - pair * blocks) * 256 + threadIdx.x;
+  if (count < 2 || i >= K * V) return;                     // (the walk of a single segment has done all of it)
+  const float lam = g.log_decay[head];
+  const int r = i / V, c = i - r * V;
+  int slot = g.slots ? g.slots[n] : n;
+  if ((unsigned)slot >= (unsigned)g.pool) slot = -1;
+  const size_t at = slot >= 0 ? ((size_t)slot * g.heads + head) * K * V + r * job.at_k + c * job.at_v : 0;
+  float s = job.state_in && slot >= 0 ? job.state_in[at] : 0.f;
+  const float keep = expf((float)g.segment * lam);
+  float* p = job.pieces + ((size_t)first * g.heads + head) * K * V + i;
+  const size_t step = (size_t)g.heads * K * V;
+  constexpr int AHEAD = 8;
+  for (int k0 = 0; k0 < count; k0 += AHEAD) {
+    float own[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) own[k] = k0 + k < count ? p[(size_t)(k0 + k) * step] : 0.f;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (k0 + k >= count) break;
+      p[(size_t)(k0 + k) * step] = s;
+      const bool last = k0 + k + 1 == count;
+      const int rows = length - (count - 1) * g.segment;
+      s = (last ? expf((float)rows * lam) : keep) * s + own[k];
+    }
+  }
+  if (job.state_out && slot >= 0) job.state_out[at] = s;
+}
+
+// Sums over the heads that share keys and values
+template <typename T> __global__ __launch_bounds__(256) void share_kernel(const float* in, T* out, long ld_out, const int* starts, int sequences, int rows, int groups, int share, int cols) {
+  const int r = blockIdx.x;
+  if (starts && (r < starts[0] || r >= starts[sequences])) return;
+  const float* p = in + (size_t)r * groups * share * cols;
+  for (int i = threadIdx.x; i < groups * cols; i += 256) {
+    const int h = i / cols, c = i - h * cols;
+    float t = 0.f;
+    for (int k = 0; k < share; ++k) t += p[(size_t)(h * share + k) * cols + c];
+    Store<T>::store1(out + (size_t)r * ld_out + i, t);
+  }
+}
+
+// ---- one row of every sequence -------------------------------------------------------------------
+
+// S <- g S + k v^T, o = scale S^T q. A workgroup a sequence and head: COLS threads for four columns of S each, 256 / COLS rows at a time; all of a thread's rows are requested before the
+// first one is needed. Bound by memory: S is read and written once.
+template <typename T, int COLS, int ROWS, bool VEC>
+__global__ __launch_bounds__(256) void step_kernel(LinearStepArgs a) {
+  constexpr int PAR = 256 / COLS;
+  __shared__ float q[LINEAR_DIM_MAX], k[LINEAR_DIM_MAX];
+  __shared__ float4 red[PAR][COLS];
+  const int n = blockIdx.x / a.heads, head = blockIdx.x - n * a.heads, K = a.K, V = a.V, tid = threadIdx.x;
+  const int c = tid % COLS * 4, p = tid / COLS;
+  int slot = a.slots ? a.slots[n] : n;
+  if ((unsigned)slot >= (unsigned)a.pool) slot = -1;
+  const size_t at = slot >= 0 ? ((size_t)slot * a.heads + head) * K * V : 0;
+  const float* in = a.state_in && slot >= 0 ? a.state_in + at : nullptr;
+  float* out = a.state_out && slot >= 0 ? a.state_out + at : nullptr;
+  auto load = [&](int r) __attribute__((always_inline)) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (in && r < K) {
+      const float* f = in + (size_t)r * V + c;
+      if (VEC) { if (c < V) s = *reinterpret_cast<const float4*>(f); }
+      else {
+        if (c < V) s.x = f[0];
+        if (c + 1 < V) s.y = f[1];
+        if (c + 2 < V) s.z = f[2];
+        if (c + 3 < V) s.w = f[3];
+      }
+    }
+    return s;
+  };
+  float4 S[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) S[i] = load(p + i * PAR);
+  for (int i = tid; i < K; i += 256) {
+    q[i] = Store<T>::load1((const T*)a.q + (size_t)n * a.ld_q + (size_t)head * K + i);
+    k[i] = Store<T>::load1((const T*)a.k + (size_t)n * a.ld_k + (size_t)(head / a.share) * K + i);
+  }
+  float v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = c + j < V ? Store<T>::load1((const T*)a.v + (size_t)n * a.ld_v + (size_t)(head / a.share) * V + c + j) : 0.f;
+  const float keep = expf(a.log_decay[head]);
+  __syncthreads();
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int r0 = 0; r0 < K; r0 += ROWS * PAR) {
+    if (r0) {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) S[i] = load(r0 + p + i * PAR);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int r = r0 + p + i * PAR;
+      if (r >= K) continue;
+      const float kr = k[r], qr = q[r];
+      float4 s = S[i];
+      s.x = keep * s.x + kr * v[0]; s.y = keep * s.y + kr * v[1]; s.z = keep * s.z + kr * v[2]; s.w = keep * s.w + kr * v[3];
+      o.x += qr * s.x; o.y += qr * s.y; o.z += qr * s.z; o.w += qr * s.w;
+      if (out) {
+        float* f = out + (size_t)r * V + c;
+        if (VEC) { if (c < V) *reinterpret_cast<float4*>(f) = s; }
+        else {
+          if (c < V) f[0] = s.x;
+          if (c + 1 < V) f[1] = s.y;
+          if (c + 2 < V) f[2] = s.z;
+          if (c + 3 < V) f[3] = s.w;
+        }
+      }
+    }
+  }
+  red[p][tid % COLS] = o;
+  __syncthreads();
+  for (int i = tid; i < V; i += 256) {
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < PAR; ++j) t += reinterpret_cast<const float*>(&red[j][0])[i];
+    Store<T>::store1((T*)a.o + (size_t)n * a.ld_o + (size_t)head * V + i, a.scale * t);
+  }
+}
+
+template <typename T, int DK, int PLANES, bool VEC, bool SUM> hipError_t walk_run(const LinearArgs& g, int jobs, hipStream_t s) {
+  constexpr int LDA = DK + Mix<T>::PAD, LDB = SLICE + Mix<T>::PAD;
+  constexpr size_t lds = (size_t)(CHUNK * LDA + CHUNK * LDB + (SUM ? 0 : Mix<T>::PLANES * SLICE * LDA)) * sizeof(T);
+  static const hipError_t allowed = hipFuncSetAttribute((const void*)walk_kernel<T, DK, PLANES, VEC, SUM>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (allowed != hipSuccess) return allowed;
+  int slices = 0;
+  for (int j = 0; j < jobs; ++j) slices = g.job[j].slices > slices ? g.job[j].slices : slices;
+  DDG_LAUNCH((walk_kernel<T, DK, PLANES, VEC, SUM>), dim3((unsigned)(g.segments * g.heads * slices + 7) / 8 * 8, jobs), dim3(256), lds, s, g);
+  return hipGetLastError();
+}
+template <typename T, int DK, bool VEC, bool SUM> hipError_t walk_planes(const LinearArgs& g, int jobs, hipStream_t s) {
+  if (sizeof(T) == 4) return walk_run<T, DK, 1, VEC, SUM>(g, jobs, s);
+  bool kept = false;
+  for (int j = 0; j < jobs; ++j) kept |= g.job[j].state_out != nullptr;
+  return kept ? walk_run<T, DK, sizeof(T) == 4 ? 1 : 3, VEC, SUM>(g, jobs, s) : walk_run<T, DK, sizeof(T) == 4 ? 1 : 2, VEC, SUM>(g, jobs, s);
+}
+template <typename T, bool VEC, bool SUM> hipError_t walk_any(const LinearArgs& g, int jobs, hipStream_t s) {
+  int most = 0;
+  for (int j = 0; j < jobs; ++j) most = g.job[j].K > most ? g.job[j].K : most;
+  return most <= 64 ? walk_planes<T, 64, VEC, SUM>(g, jobs, s) : most <= 128 ? walk_planes<T, 128, VEC, SUM>(g, jobs, s) : walk_planes<T, 256, VEC, SUM>(g, jobs, s);
+}
+bool whole(const void* p, long ld, int dim, size_t size) { return (uintptr_t)p % 16 == 0 && (size_t)ld * size % 16 == 0 && (size_t)dim * size % 16 == 0; }
+template <typename T> hipError_t walk_typed(const LinearArgs& g, int jobs, hipStream_t s) {
+  bool vec = true;
+  for (int i = 0; i < jobs; ++i) {
+    const LinearJob& j = g.job[i];
+    vec &= whole(j.x, j.ld_x, j.K, sizeof(T)) && whole(j.a, j.ld_a, j.K, sizeof(T)) && whole(j.b, j.ld_b, j.V, sizeof(T)) &&
+           whole(j.out, j.ld_out, j.V, j.out_f32 ? 4 : sizeof(T));
+  }
+  if (g.split) {
+    hipError_t e = vec ? walk_any<T, true, true>(g, jobs, s) : walk_any<T, false, true>(g, jobs, s);
+    if (e != hipSuccess) return e;
+    int most = 0;
+    for (int i = 0; i < jobs; ++i) most = g.job[i].K * g.job[i].V > most ? g.job[i].K * g.job[i].V : most;
+    const int blocks = (most + 255) / 256;
+    DDG_LAUNCH(scan_kernel, dim3(blocks * g.sequences * g.heads, jobs), dim3(256), 0, s, g, blocks);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return vec ? walk_any<T, true, false>(g, jobs, s) : walk_any<T, false, false>(g, jobs, s);
+}
+
+template <typename T, int COLS, int ROWS> hipError_t step_run(const LinearStepArgs& a, bool vec, hipStream_t s) {
+  if (vec) DDG_LAUNCH((step_kernel<T, COLS, ROWS, true>), dim3(a.rows * a.heads), dim3(256), 0, s, a);
+  else DDG_LAUNCH((step_kernel<T, COLS, ROWS, false>), dim3(a.rows * a.heads), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T> hipError_t step_typed(const LinearStepArgs& a, hipStream_t s) {
+  const bool vec = a.V % 4 == 0 && (uintptr_t)a.state_in % 16 == 0 && (uintptr_t)a.state_out % 16 == 0;
+  if (a.V <= 64) return step_run<T, 16, 8>(a, vec, s);
+  if (a.V <= 128) return step_run<T, 32, 16>(a, vec, s);
+  return step_run<T, 64, 16>(a, vec, s);
+}
+
+}  // namespace
+
+int linear_segment(int rows, int sequences, int walks, bool ragged) {
+  const long most = 1024 / walks;                          // segments that fill the chip
+  if (sequences >= most && !ragged) return 0;
+  long segment = (rows + most - 1) / (most > 0 ? most : 1);
+  segment = (segment + CHUNK - 1) / CHUNK * CHUNK;
+  segment = segment < 256 ? 256 : segment > 2048 ? 2048 : segment;
+  const long length = ragged ? rows : rows / sequences;
+  return length <= segment ? 0 : (int)segment;
+}
+
+hipError_t linear_launch(const LinearArgs& a, int jobs, hipStream_t s) { return a.dtype == BF16 ? walk_typed<bf16_t>(a, jobs, s) : walk_typed<float>(a, jobs, s); }
+
+hipError_t linear_step_launch(const LinearStepArgs& a, hipStream_t s) { return a.dtype == BF16 ? step_typed<bf16_t>(a, s) : step_typed<float>(a, s); }
+
+hipError_t linear_share_launch(const float* in, void* out, long ld_out, const int* starts, int sequences, int rows, int groups, int share, int cols, int dtype,
+                               hipStream_t s) {
+  if (dtype == BF16) DDG_LAUNCH(share_kernel<bf16_t>, dim3(rows), dim3(256), 0, s, in, (bf16_t*)out, ld_out, starts, sequences, rows, groups, share, cols);
+  else DDG_LAUNCH(share_kernel<float>, dim3(rows), dim3(256), 0, s, in, (float*)out, ld_out, starts, sequences, rows, groups, share, cols);
+  return hipGetLastError();
+}
+
+}  // namespace ddg

@@ -57,6 +57,24 @@ class VocabDesc(C.Structure):
                 ("stream", C.c_void_p), ("dry_run", C.c_int), ("unaligned", C.c_int)]
 
 
+class RotaryDesc(C.Structure):
+    _fields_ = [("rows", C.c_int), ("heads", C.c_int), ("dim", C.c_int), ("dtype", C.c_int), ("rot", C.c_int), ("interleaved", C.c_int),
+                ("base", C.c_double), ("factor", C.c_double), ("context", C.c_double), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_float),
+                ("ld_x", C.c_long), ("ld_y", C.c_long), ("stream", C.c_void_p), ("dry_run", C.c_int)]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [("rows", C.c_int), ("sequences", C.c_int), ("heads", C.c_int), ("kv_heads", C.c_int), ("dim_k", C.c_int), ("dim_v", C.c_int),
+                ("dtype", C.c_int), ("slots", C.c_int), ("scale", C.c_float), ("ld_q", C.c_long), ("ld_k", C.c_long), ("ld_v", C.c_long), ("ld_o", C.c_long),
+                ("stream", C.c_void_p), ("dry_run", C.c_int)]
+
+
+class GatedJoinDesc(C.Structure):
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int), ("dtype", C.c_int), ("eps", C.c_float), ("scale", C.c_float), ("residual_scale", C.c_float),
+                ("group", C.c_int), ("gate", C.c_int), ("ld_y", C.c_long), ("ld_gate", C.c_long), ("ld_residual", C.c_long), ("ld_x", C.c_long),
+                ("ld_out", C.c_long), ("stream", C.c_void_p), ("dry_run", C.c_int)]
+
+
 _lib = None
 
 
@@ -133,6 +151,15 @@ def load_library():
         "ddg_join_norm_backward": (st, [C.POINTER(JoinDesc), C.c_uint64] + [vp] * 9 + [C.c_size_t]),
         "ddg_vocab_loss_workspace": (C.c_size_t, [C.POINTER(VocabDesc), C.c_int]),
         "ddg_vocab_loss": (st, [C.POINTER(VocabDesc)] + [vp] * 10 + [C.c_size_t]),
+        "ddg_rotary_table": (st, [C.POINTER(RotaryDesc), vp]),
+        "ddg_rotary": (st, [C.POINTER(RotaryDesc), vp, vp, C.c_long, vp, C.c_int, vp]),
+        "ddg_linear_attention_workspace": (C.c_size_t, [C.POINTER(LinearDesc), C.c_int]),
+        "ddg_linear_attention": (st, [C.POINTER(LinearDesc)] + [vp] * 10 + [C.c_size_t]),
+        "ddg_linear_attention_backward": (st, [C.POINTER(LinearDesc)] + [vp] * 14 + [C.c_size_t]),
+        "ddg_linear_attention_step": (st, [C.POINTER(LinearDesc)] + [vp] * 8),
+        "ddg_gated_join": (st, [C.POINTER(GatedJoinDesc)] + [vp] * 9),
+        "ddg_gated_join_workspace": (C.c_size_t, [C.POINTER(GatedJoinDesc)]),
+        "ddg_gated_join_backward": (st, [C.POINTER(GatedJoinDesc)] + [vp] * 15 + [C.c_size_t]),
         "ddg_last_error": (C.c_char_p, []),
         "ddg_version": (C.c_char_p, []),
     }
@@ -158,6 +185,8 @@ EXPORTS = ["ddg_module_create", "ddg_module_destroy", "ddg_param_count", "ddg_ou
            "ddg_pipeline_set_mail",
            "ddg_dropout", "ddg_join_norm", "ddg_join_norm_q8", "ddg_join_norm_workspace", "ddg_join_norm_backward",
            "ddg_vocab_loss_workspace", "ddg_vocab_loss",
+           "ddg_rotary_table", "ddg_rotary", "ddg_linear_attention_workspace", "ddg_linear_attention", "ddg_linear_attention_backward",
+           "ddg_linear_attention_step", "ddg_gated_join", "ddg_gated_join_workspace", "ddg_gated_join_backward",
            "ddg_last_error", "ddg_version"]
 
 
@@ -525,5 +554,102 @@ class VocabLoss:
         _int32(targets, "targets")
         status = self._call(self._d, _ptr(h), _ptr(w), _ptr(targets), _ptr(weights), _ptr(loss), _ptr(row_loss), _ptr(lse), _ptr(dh),
                             _ptr(dw), _ptr(workspace), _bytes(workspace))
+        if status:
+            _check(status)
+
+
+class Rotary:
+    """ddg_rotary on [rows][heads * dim]; inverse=True on the error gradient is its backward pass. `table` is what table() returns, copied to
+    the device once; its 64-bit words may be of any 8-byte type there."""
+
+    def __init__(self, rows, heads, dim, dtype, rot=0, interleaved=False, base=10000.0, factor=1.0, context=0, low=1.0, high=32.0, magnitude=1.0, ld_x=0,
+                 ld_y=0, stream=None, dry_run=False):
+        self.desc = RotaryDesc(rows, heads, dim, dtype, rot, 1 if interleaved else 0, base, factor, context, low, high, magnitude, ld_x, ld_y, stream,
+                               1 if dry_run else 0)
+        lib = load_library()
+        self._d, self._call, self._table = C.byref(self.desc), lib.ddg_rotary, lib.ddg_rotary_table
+
+    def table(self) -> np.ndarray:
+        """The frequencies as 64-bit fractions of a turn, on the host."""
+        out = np.empty(max(1, (self.desc.rot or self.desc.dim) // 2), np.uint64)
+        _check(self._table(self._d, _ptr(out)))
+        return out
+
+    def __call__(self, x, y, table, positions=None, first=0, inverse=False):
+        _int32(positions, "positions")
+        status = self._call(self._d, _ptr(x), _ptr(positions), first, _ptr(table), 1 if inverse else 0, _ptr(y))
+        if status:
+            _check(status)
+
+
+class LinearAttention:
+    """Linear attention with a decay for each head: ddg_linear_attention, ddg_linear_attention_backward, ddg_linear_attention_step."""
+
+    def __init__(self, rows, heads, dim_k, dim_v, dtype, sequences=1, kv_heads=0, scale=None, slots=0, ld_q=0, ld_k=0, ld_v=0, ld_o=0, stream=None,
+                 dry_run=False):
+        if scale is None:
+            scale = dim_k ** -0.5 if dim_k > 0 else 1.0
+        self.desc = LinearDesc(rows, sequences, heads, kv_heads, dim_k, dim_v, dtype, slots, scale, ld_q, ld_k, ld_v, ld_o, stream, 1 if dry_run else 0)
+        lib = load_library()
+        self._d, self._space = C.byref(self.desc), lib.ddg_linear_attention_workspace
+        self._forward, self._backward, self._step = lib.ddg_linear_attention, lib.ddg_linear_attention_backward, lib.ddg_linear_attention_step
+
+    def workspace_bytes(self, backward=False) -> int:
+        return int(self._space(self._d, 1 if backward else 0))
+
+    def forward(self, q, k, v, log_decay, o, starts=None, slots=None, state_in=None, state_out=None, workspace=None):
+        _int32(starts, "starts")
+        _int32(slots, "slots")
+        status = self._forward(self._d, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(starts), _ptr(slots), _ptr(state_in), _ptr(o), _ptr(state_out),
+                               _ptr(workspace), _bytes(workspace))
+        if status:
+            _check(status)
+
+    def backward(self, q, k, v, log_decay, d_o, dq=None, dk=None, dv=None, starts=None, slots=None, state_in=None, d_state_out=None, d_state_in=None,
+                 workspace=None):
+        _int32(starts, "starts")
+        _int32(slots, "slots")
+        status = self._backward(self._d, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(starts), _ptr(slots), _ptr(state_in), _ptr(d_o), _ptr(d_state_out),
+                                _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_state_in), _ptr(workspace), _bytes(workspace))
+        if status:
+            _check(status)
+
+    def step(self, q, k, v, log_decay, o, slots=None, state_in=None, state_out=None):
+        """One row of every sequence."""
+        _int32(slots, "slots")
+        status = self._step(self._d, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(slots), _ptr(state_in), _ptr(o), _ptr(state_out))
+        if status:
+            _check(status)
+
+
+GATES = {"none": 0, "column": 1, "plain": 2, "sigmoid": 3, "silu": 4}
+
+
+class GatedJoin:
+    """Norm after a block, its gate, the residual and the norm before the next block: ddg_gated_join, ddg_gated_join_backward. gate: a key of GATES."""
+
+    def __init__(self, rows, cols, dtype, eps=1e-6, gate="none", group=0, scale=1.0, residual_scale=1.0, ld_y=0, ld_gate=0, ld_residual=0, ld_x=0, ld_out=0,
+                 stream=None, dry_run=False):
+        if gate not in GATES:
+            raise DDGError(1, f"gate must be one of {', '.join(GATES)} ({gate!r})")
+        self.desc = GatedJoinDesc(rows, cols, dtype, eps, scale, residual_scale, group, GATES[gate], ld_y, ld_gate, ld_residual, ld_x, ld_out, stream,
+                                  1 if dry_run else 0)
+        lib = load_library()
+        self._d, self._space = C.byref(self.desc), lib.ddg_gated_join_workspace
+        self._forward, self._backward = lib.ddg_gated_join, lib.ddg_gated_join_backward
+
+    def workspace_bytes(self) -> int:
+        """Bytes that `backward` needs for sums over rows."""
+        return int(self._space(self._d))
+
+    def forward(self, y, gate, residual, gain_y, gain_x, x_out=None, out=None, rstd_y=None, rstd_x=None):
+        status = self._forward(self._d, _ptr(y), _ptr(gate), _ptr(residual), _ptr(gain_y), _ptr(gain_x), _ptr(x_out), _ptr(out), _ptr(rstd_y), _ptr(rstd_x))
+        if status:
+            _check(status)
+
+    def backward(self, y, rstd_y, gate, x, rstd_x, gain_y, gain_x, d_out=None, d_x=None, d_residual=None, d_y=None, d_gate=None, d_gain_y=None, d_gain_x=None,
+                 workspace=None):
+        status = self._backward(self._d, _ptr(y), _ptr(rstd_y), _ptr(gate), _ptr(x), _ptr(rstd_x), _ptr(gain_y), _ptr(gain_x), _ptr(d_out), _ptr(d_x),
+                                _ptr(d_residual), _ptr(d_y), _ptr(d_gate), _ptr(d_gain_y), _ptr(d_gain_x), _ptr(workspace), _bytes(workspace))
         if status:
             _check(status)
