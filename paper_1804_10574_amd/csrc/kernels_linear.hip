@@ -75,22 +75,71 @@ template <int N> __device__ __forceinline__ void weigh(float4 b, const float* w,
   o[0] = make_float4(b.x * w[0], b.y * w[1], b.z * w[2], b.w * w[3]);
 }
 
-// 16 bytes of n elements (n may be 0 or less: zeros)
-template <typename T, bool VEC> __device__ __forceinline__ typename Mma<T>::frag_t piece(const T* p, int n) {
+// The rows of a chunk of one operand, and 16 bytes of a row, zeros where there is nothing: no load is conditional, since where branches meet the compiler waits for
+// all loads in flight. VEC: whole 16-byte pieces through a resource, what lies outside at NOWHERE. Otherwise pieces wherever they begin, from the nearest place that
+// has them (the first row, the end of the row), put right by settle() when they are needed.
+template <typename T, bool VEC> struct Rows;
+template <typename T> struct Rows<T, true> {
   typedef typename Mma<T>::frag_t frag_t;
-  frag_t v = Mma<T>::zero();
-  if (VEC) {
-    if (n > 0) v = *reinterpret_cast<const frag_t*>(p);
-  } else if (n >= Mma<T>::KV) {
-    __builtin_memcpy(&v, p, sizeof(v));
-  } else if (n > 0) {
-    T e[Mma<T>::KV];
-#pragma unroll
-    for (int i = 0; i < Mma<T>::KV; ++i) e[i] = i < n ? p[i] : T{};
-    __builtin_memcpy(&v, e, sizeof(v));
+  wide_rsrc_t res;
+  unsigned step, top;
+  int n, cols;
+  // row r of the chunk is at p + r * stride; n rows of `cols` columns
+  __device__ __forceinline__ void at(const T* p, long stride, int n_, int cols_) {
+    const bool back = stride < 0;
+    const uint64_t q = (uint64_t)(uintptr_t)(back ? p + (CHUNK - 1) * stride : p);
+    const uint64_t u = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)q) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(q >> 32)) << 32;
+    res = wide_rsrc((const void*)(uintptr_t)u, 0x80000000u);
+    const unsigned by = (unsigned)((back ? -stride : stride) * (long)sizeof(T));
+    step = back ? 0u - by : by;
+    top = back ? (CHUNK - 1) * by : 0u;
+    n = n_; cols = cols_;
   }
-  return v;
-}
+  __device__ __forceinline__ frag_t get(int r, int c) const {
+    return __builtin_bit_cast(frag_t, wide_load(res, r < n && c < cols ? top + (unsigned)r * step + (unsigned)c * (unsigned)sizeof(T) : NOWHERE, 0));
+  }
+  __device__ __forceinline__ frag_t settle(frag_t v, int, int) const { return v; }
+};
+template <typename T> struct Rows<T, false> {
+  typedef typename Mma<T>::frag_t frag_t;
+  static constexpr int W = Mma<T>::KV;
+  const T* p;
+  long stride;
+  int n, cols;
+  __device__ __forceinline__ void at(const T* p_, long stride_, int n_, int cols_) { p = p_; stride = stride_; n = n_; cols = cols_; }
+  __device__ __forceinline__ frag_t get(int r, int c) const {
+    const T* row = p + (r < n ? r : 0) * stride;
+    frag_t v;
+    if (cols >= W) {
+      __builtin_memcpy(&v, row + (c + W <= cols ? c : cols - W), sizeof(v));
+    } else {
+      T e[W];
+#pragma unroll
+      for (int i = 0; i < W; ++i) e[i] = row[i < cols ? i : 0];
+      __builtin_memcpy(&v, e, sizeof(v));
+    }
+    return v;
+  }
+  __device__ __forceinline__ frag_t settle(frag_t f, int r, int c) const {
+    const uint4 v = __builtin_bit_cast(uint4, f);
+    uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+    if (r >= n || c >= cols) lo = hi = 0;
+    if (cols >= W) {                                       // what was read began `past` elements before c
+      const int past = c + W <= cols ? 0 : c - (cols - W), bits = (past * (int)sizeof(T) & 7) * 8;
+      if (past * (int)sizeof(T) >= 8) { lo = hi; hi = 0; }
+      lo = lo >> bits | (bits ? hi << (64 - bits) : 0);
+      hi >>= bits;
+    } else {
+      const int bits = cols * (int)sizeof(T) * 8;          // c is 0
+      hi = bits > 64 ? hi & ((1ull << (bits - 64)) - 1) : 0;
+      if (bits < 64) lo &= (1ull << bits) - 1;
+    }
+    return __builtin_bit_cast(frag_t, make_uint4((unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)));
+  }
+};
+
+// What LDS holds is there for all waves; loads and stores of memory go on
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Where a workgroup is: its sequence, and the rows [first, first + rows) of it, counted in the direction of the walk
 struct Place { int sequence, start, length, first, rows, segments; bool none; };
@@ -152,7 +201,7 @@ __device__ __forceinline__ int on_die(int id, int total) {
 
 // SUM: only the state of the segment's own rows, for the scan. PLANES: fragments a weighted b is taken apart into.
 template <typename T, int DK, int PLANES, bool VEC, bool SUM>
-__global__ __launch_bounds__(256) void walk_kernel(LinearArgs g) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk_kernel(LinearArgs g) {
   typedef Mma<T> M;
   typedef Mix<T> X;
   typedef typename M::frag_t frag_t;
@@ -193,13 +242,21 @@ __global__ __launch_bounds__(256) void walk_kernel(LinearArgs g) {
     } else if (!SUM && job.state_in && slot >= 0) {
       from = job.state_in + ((size_t)slot * g.heads + head) * K * V;
     }
+    if (from) {
+      from += (col < V ? col : V - 1) * rv;
+#pragma unroll
+      for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 16 * t + 4 * l4 + e;
+          S[t][e] = from[(r < K ? r : K - 1) * rk];
+        }
+    }
 #pragma unroll
     for (int t = 0; t < DK / 16; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 16 * t + 4 * l4 + e;
-        S[t][e] = from && r < K && col < V ? from[r * rk + col * rv] : 0.f;
-      }
+      for (int e = 0; e < 4; ++e)
+        if (!from || 16 * t + 4 * l4 + e >= K || col >= V) S[t][e] = 0.f;
   }
   __syncthreads();
 
@@ -224,40 +281,35 @@ __global__ __launch_bounds__(256) void walk_kernel(LinearArgs g) {
   const T* const bb = (const T*)job.b + origin * job.ld_b + (size_t)(head / job.share_b) * V + place.first * sb + v0;
 
   frag_t xr[STEPS], ar[PA], br[PB];
+  Rows<T, VEC> rx, ra, rb;
   auto request = [&](int r0) __attribute__((always_inline)) {
+    const int n = min(CHUNK, place.rows - r0);
     if (!SUM) {
-      const bool in = r0 + row < place.rows;
+      rx.at(bx + r0 * sx, sx, n, K);
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        const int c = s * M::KSTEP + l4 * W;
-        xr[s] = piece<T, VEC>(bx + (r0 + row) * sx + c, in ? K - c : 0);
-      }
+      for (int s = 0; s < STEPS; ++s) xr[s] = rx.get(row, s * M::KSTEP + l4 * W);
     }
+    ra.at(ba + r0 * sa, sa, n, K);
 #pragma unroll
-    for (int i = 0; i < PA; ++i) {
-      const int p = tid + i * 256, r = p / (DK / W), c = p % (DK / W) * W;
-      ar[i] = piece<T, VEC>(ba + (r0 + r) * sa + c, r0 + r < place.rows ? K - c : 0);
-    }
+    for (int i = 0; i < PA; ++i) ar[i] = ra.get((tid + i * 256) / (DK / W), (tid + i * 256) % (DK / W) * W);
+    rb.at(bb + r0 * sb, sb, n, V - v0);
 #pragma unroll
-    for (int i = 0; i < PB; ++i) {
-      const int p = tid + i * 256, r = p / (SLICE / W), c = p % (SLICE / W) * W;
-      br[i] = piece<T, VEC>(bb + (r0 + r) * sb + c, r0 + r < place.rows ? V - v0 - c : 0);
-    }
+    for (int i = 0; i < PB; ++i) br[i] = rb.get((tid + i * 256) / (SLICE / W), (tid + i * 256) % (SLICE / W) * W);
   };
 
   if (place.rows > 0) request(0);
   for (int r0 = 0; r0 < place.rows; r0 += CHUNK) {
     const int n = min(CHUNK, place.rows - r0);
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int i = 0; i < PA; ++i) {
       const int p = tid + i * 256, r = p / (DK / W), c = p % (DK / W) * W;
-      *reinterpret_cast<frag_t*>(at + r * LDA + c) = ar[i];
+      *reinterpret_cast<frag_t*>(at + r * LDA + c) = ra.settle(ar[i], r, c);
     }
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       const int p = tid + i * 256, r = p / (SLICE / W), c = p % (SLICE / W) * W;
-      *reinterpret_cast<frag_t*>(bt + r * LDB + c) = br[i];
+      *reinterpret_cast<frag_t*>(bt + r * LDB + c) = rb.settle(br[i], r, c);
     }
     if (!SUM) {
       T* const to = st + (16 * wave + l16) * LDA + 4 * l4;
@@ -273,11 +325,11 @@ __global__ __launch_bounds__(256) void walk_kernel(LinearArgs g) {
         }
       }
     }
-    __syncthreads();
+    lds_barrier();
     frag_t x[STEPS];
     if (!SUM) {
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) x[s] = xr[s];
+      for (int s = 0; s < STEPS; ++s) x[s] = rx.settle(xr[s], row, s * M::KSTEP + l4 * W);
     }
     if (r0 + CHUNK < place.rows) request(r0 + CHUNK);
     if (!SUM) {
@@ -404,7 +456,7 @@ __global__ __launch_bounds__(256) void scan_kernel(LinearArgs g, int blocks) {
   for (int k0 = 0; k0 < count; k0 += AHEAD) {
     float own[AHEAD];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) own[k] = k0 + k < count ? p[(size_t)(k0 + k) * step] : 0.f;
+    for (int k = 0; k < AHEAD; ++k) own[k] = p[(size_t)min(k0 + k, count - 1) * step];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       if (k0 + k >= count) break;
@@ -519,17 +571,23 @@ template <typename T, int DK, int PLANES, bool VEC, bool SUM> hipError_t walk_ru
   return hipGetLastError();
 }
 template <typename T, int DK, bool VEC, bool SUM> hipError_t walk_planes(const LinearArgs& g, int jobs, hipStream_t s) {
-  if (sizeof(T) == 4) return walk_run<T, DK, 1, VEC, SUM>(g, jobs, s);
-  bool kept = false;
-  for (int j = 0; j < jobs; ++j) kept |= g.job[j].state_out != nullptr;
-  return kept ? walk_run<T, DK, sizeof(T) == 4 ? 1 : 3, VEC, SUM>(g, jobs, s) : walk_run<T, DK, sizeof(T) == 4 ? 1 : 2, VEC, SUM>(g, jobs, s);
+  if constexpr (sizeof(T) == 4) {
+    return walk_run<T, DK, 1, VEC, SUM>(g, jobs, s);
+  } else {
+    bool kept = false;
+    for (int j = 0; j < jobs; ++j) kept |= g.job[j].state_out != nullptr;
+    return kept ? walk_run<T, DK, 3, VEC, SUM>(g, jobs, s) : walk_run<T, DK, 2, VEC, SUM>(g, jobs, s);
+  }
 }
 template <typename T, bool VEC, bool SUM> hipError_t walk_any(const LinearArgs& g, int jobs, hipStream_t s) {
   int most = 0;
   for (int j = 0; j < jobs; ++j) most = g.job[j].K > most ? g.job[j].K : most;
   return most <= 64 ? walk_planes<T, 64, VEC, SUM>(g, jobs, s) : most <= 128 ? walk_planes<T, 128, VEC, SUM>(g, jobs, s) : walk_planes<T, 256, VEC, SUM>(g, jobs, s);
 }
-bool whole(const void* p, long ld, int dim, size_t size) { return (uintptr_t)p % 16 == 0 && (size_t)ld * size % 16 == 0 && (size_t)dim * size % 16 == 0; }
+// Pieces of 16 bytes, and a chunk of rows inside the 31 bits of an offset
+bool whole(const void* p, long ld, int dim, size_t size) {
+  return (uintptr_t)p % 16 == 0 && (size_t)ld * size % 16 == 0 && (size_t)dim * size % 16 == 0 && (size_t)ld * size < (1u << 31) / CHUNK;
+}
 template <typename T> hipError_t walk_typed(const LinearArgs& g, int jobs, hipStream_t s) {
   bool vec = true;
   for (int i = 0; i < jobs; ++i) {
@@ -564,14 +622,16 @@ template <typename T> hipError_t step_typed(const LinearStepArgs& a, hipStream_t
 
 }  // namespace
 
+// Two workgroups a compute unit are resident: fewer walks than that are cut. Ragged sequences: nobody knows how long the longest is, and one of all the rows is allowed for.
 int linear_segment(int rows, int sequences, int walks, bool ragged) {
-  const long most = 1024 / walks;                          // segments that fill the chip
-  if (sequences >= most && !ragged) return 0;
-  long segment = (rows + most - 1) / (most > 0 ? most : 1);
+  const int length = ragged ? rows : rows / sequences;
+  const long have = (long)sequences * walks, most = have < 512 ? (512 + have - 1) / have : 1;     // segments a sequence of average length
+  const int average = rows / sequences;
+  int segment = (int)((average + most - 1) / most);
   segment = (segment + CHUNK - 1) / CHUNK * CHUNK;
-  segment = segment < 256 ? 256 : segment > 2048 ? 2048 : segment;
-  const long length = ragged ? rows : rows / sequences;
-  return length <= segment ? 0 : (int)segment;
+  segment = segment < 256 ? 256 : segment;
+  if (ragged && segment > 2048) segment = 2048;
+  return length <= segment || (!ragged && most == 1) ? 0 : segment;
 }
 
 hipError_t linear_launch(const LinearArgs& a, int jobs, hipStream_t s) { return a.dtype == BF16 ? walk_typed<bf16_t>(a, jobs, s) : walk_typed<float>(a, jobs, s); }
