@@ -9,12 +9,15 @@
 #include "ddg_device.h"
 #include "ddg_mixing.h"
 
+#include <type_traits>
+
 namespace ddg {
 namespace {
 
 constexpr int CHUNK = 64, SLICE = 64;
 
 typedef short tr4_t __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 typedef tr4_t __attribute__((address_space(3))) * tr_ptr_t;
 
 // What the two types do differently. A fragment holds KV consecutive values of the contracted index for one row or column (Mma in ddg_device.h).
@@ -86,14 +89,18 @@ template <typename T> struct Rows<T, true> {
   int n, cols;
   // row r of the chunk is at p + r * stride; n rows of `cols` columns
   __device__ __forceinline__ void at(const T* p, long stride, int n_, int cols_) {
+    over(p, 0, stride, sizeof(T));
+    n = n_; cols = cols_;
+  }
+  // the same at element `from` of p, of elements of `size` bytes; p null: nowhere
+  __device__ __forceinline__ void over(const void* p, long from, long stride, int size) {
     const bool back = stride < 0;
-    const uint64_t q = (uint64_t)(uintptr_t)(back ? p + (CHUNK - 1) * stride : p);
+    const uint64_t q = (uint64_t)(uintptr_t)p + (uint64_t)((back ? from + (CHUNK - 1) * stride : from) * size);
     const uint64_t u = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)q) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(q >> 32)) << 32;
-    res = wide_rsrc((const void*)(uintptr_t)u, 0x80000000u);
-    const unsigned by = (unsigned)((back ? -stride : stride) * (long)sizeof(T));
+    res = wide_rsrc((const void*)(uintptr_t)u, p ? 0x80000000u : 0u);
+    const unsigned by = (unsigned)((back ? -stride : stride) * size);
     step = back ? 0u - by : by;
     top = back ? (CHUNK - 1) * by : 0u;
-    n = n_; cols = cols_;
   }
   __device__ __forceinline__ frag_t get(int r, int c) const {
     return __builtin_bit_cast(frag_t, wide_load(res, r < n && c < cols ? top + (unsigned)r * step + (unsigned)c * (unsigned)sizeof(T) : NOWHERE, 0));
@@ -206,7 +213,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
   typedef Mix<T> X;
   typedef typename M::frag_t frag_t;
   constexpr int W = M::KV, LDA = DK + X::PAD, LDB = SLICE + X::PAD, STEPS = DK / M::KSTEP, OVER = 4 / X::TILES;
-  constexpr int SPLANES = X::PLANES;                       // of S as an operand
   constexpr int PA = CHUNK * DK / W / 256, PB = CHUNK * SLICE / W / 256;
   extern __shared__ __align__(16) unsigned char smem[];
   T* const at = reinterpret_cast<T*>(smem);                // [64][LDA]
@@ -215,7 +221,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
   __shared__ float power[CHUNK + 2];
   __shared__ int counted[4];
 
-  const LinearJob& job = g.job[blockIdx.y];
+  const LinearJob job = g.job[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
   const int total = g.segments * g.heads * job.slices;
   if ((int)blockIdx.x >= total) return;
@@ -279,6 +285,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
   const T* const bx = (const T*)job.x + origin * job.ld_x + (size_t)(head / job.share_x) * K + place.first * sx;
   const T* const ba = (const T*)job.a + origin * job.ld_a + (size_t)(head / job.share_a) * K + place.first * sa;
   const T* const bb = (const T*)job.b + origin * job.ld_b + (size_t)(head / job.share_b) * V + place.first * sb + v0;
+  const long out_step = job.back ? -job.ld_out : job.ld_out, out_at = (long)origin * job.ld_out + (long)head * V + place.first * out_step;
+  const int out_size = job.out_f32 ? 4 : (int)sizeof(T);
 
   frag_t xr[STEPS], ar[PA], br[PB];
   Rows<T, VEC> rx, ra, rb;
@@ -333,52 +341,70 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
     }
     if (r0 + CHUNK < place.rows) request(r0 + CHUNK);
     if (!SUM) {
-      // pairs of rows: this wave's 16 rows as columns, the rows before them as rows
-      f32x4_t P[4];
+      // columns of the result, 16 at a time and four at once, so that no product waits for the one before: from the state
+      f32x4_t o[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        P[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (t > wave) continue;
+      for (int t = 0; t < 4; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) P[t] = M::mma(M::load(at + (16 * t + l16) * LDA + s * M::KSTEP + l4 * W), x[s], P[t]);
+      for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) P[t][e] = 16 * t + 4 * l4 + e <= row ? P[t][e] * pairs[t][e] : 0.f;
-      }
-      frag_t pairs_of[OVER][X::PLANES];
+        for (int p = 0; p < X::PLANES; ++p)
 #pragma unroll
-      for (int s = 0; s < OVER; ++s) X::pack(P + s * X::TILES, pairs_of[s]);
-      // columns of the result, 16 at a time: from the state, then from the pairs
+          for (int t = 0; t < 4; ++t) o[t] = M::mma(M::load(st + (p * SLICE + 16 * t + l16) * LDA + s * M::KSTEP + l4 * W), x[s], o[t]);
 #pragma unroll
-      for (int t = 0; t < SLICE / 16; ++t) {
-        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int p = 0; p < SPLANES; ++p)
+        for (int e = 0; e < 4; ++e) o[t][e] *= into;
+      // and from the pairs of rows: this wave's 16 rows as columns, theirs and the 16-row tiles before as rows
+      const auto mix = [&](auto tiles) __attribute__((always_inline)) {
+        constexpr int NT = decltype(tiles)::value, USED = (NT + X::TILES - 1) / X::TILES;
+        f32x4_t P[USED * X::TILES];
 #pragma unroll
-          for (int s = 0; s < STEPS; ++s) o = M::mma(M::load(st + (p * SLICE + 16 * t + l16) * LDA + s * M::KSTEP + l4 * W), x[s], o);
+        for (int t = 0; t < USED * X::TILES; ++t) P[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] *= into;
+        for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-        for (int s = 0; s < OVER; ++s) {
-          if (s * X::TILES > wave) continue;
-          const frag_t b = X::across(bt, LDB, s, 16 * t, lane);
+          for (int t = 0; t < NT; ++t) P[t] = M::mma(M::load(at + (16 * t + l16) * LDA + s * M::KSTEP + l4 * W), x[s], P[t]);
 #pragma unroll
-          for (int p = 0; p < X::PLANES; ++p) o = M::mma(b, pairs_of[s][p], o);
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) P[t][e] = t + 1 < NT || 4 * l4 + e <= l16 ? P[t][e] * pairs[t][e] : 0.f;      // (later rows may hold anything)
+#pragma unroll
+        for (int s = 0; s < USED; ++s) {
+          frag_t of[X::PLANES], b[4];
+          X::pack(P + s * X::TILES, of);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) b[t] = X::across(bt, LDB, s, 16 * t, lane);
+#pragma unroll
+          for (int p = 0; p < X::PLANES; ++p)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) o[t] = M::mma(b[t], of[p], o[t]);
         }
-        const int c = v0 + 16 * t + 4 * l4;
-        if (job.out && row < n && c < V) {
-          const size_t r = (size_t)((long)origin + (long)(place.first + r0 + row) * (job.back ? -1 : 1)), at_out = r * job.ld_out + (size_t)head * V + c;
-          if (sizeof(T) == 2 && !job.out_f32) {
-            if (VEC) Store<bf16_t>::store4((bf16_t*)job.out + at_out, o[0], o[1], o[2], o[3]);
-            else
+      };
+      if (wave == 0) mix(std::integral_constant<int, 1>());
+      else if (wave == 1) mix(std::integral_constant<int, 2>());
+      else if (wave == 2) mix(std::integral_constant<int, 3>());
+      else mix(std::integral_constant<int, 4>());
+      const int c = v0 + 4 * l4;
+      if constexpr (VEC) {
+        Rows<float, true> to;                              // (offsets in bytes; nothing is written where there is no result)
+        to.over(job.out, out_at + r0 * out_step, out_step, out_size);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) if (c + e < V) Store<bf16_t>::store1((bf16_t*)job.out + at_out + e, o[e]);
-          } else {
-            if (VEC) Store<float>::store4((float*)job.out + at_out, o[0], o[1], o[2], o[3]);
-            else
-#pragma unroll
-              for (int e = 0; e < 4; ++e) if (c + e < V) ((float*)job.out)[at_out + e] = o[e];
-          }
+        for (int t = 0; t < 4; ++t) {
+          const unsigned off = row < n && c + 16 * t < V ? to.top + (unsigned)row * to.step + (unsigned)((16 * t + c) * out_size) : NOWHERE;
+          if (out_size == 2) __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{f32x2_to_bf16x2(o[t][0], o[t][1]), f32x2_to_bf16x2(o[t][2], o[t][3])}, to.res, off, 0, 0);
+          else wide_store(to.res, __builtin_bit_cast(uint4, o[t]), off);
         }
+      } else if (job.out && row < n) {
+        const long at_row = out_at + (r0 + row) * out_step + c;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + 16 * t + e < V) {
+              if (out_size == 2) Store<bf16_t>::store1((bf16_t*)job.out + at_row + 16 * t + e, o[t][e]);
+              else ((float*)job.out)[at_row + 16 * t + e] = o[t][e];
+            }
       }
     }
     // the state after these rows
@@ -401,10 +427,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
       frag_t w[PLANES];
       weigh<PLANES>(X::across(bt, LDB, s, 16 * wave, lane), weight + 4 * X::TILES * s, w);
 #pragma unroll
-      for (int t = 0; t < DK / 16; ++t) {
-        const frag_t a = X::across(at, LDA, s, 16 * t, lane);
+      for (int t = 0; t < DK / 16; t += 4) {
+        frag_t a[4];
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p) S[t] = M::mma(a, w[p], S[t]);
+        for (int i = 0; i < 4; ++i) a[i] = X::across(at, LDA, s, 16 * (t + i), lane);
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S[t + i] = M::mma(a[i], w[p], S[t + i]);
       }
     }
   }
