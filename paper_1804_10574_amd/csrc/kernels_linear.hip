@@ -26,7 +26,7 @@ typedef tr4_t __attribute__((address_space(3))) * tr_ptr_t;
 template <typename T> struct Mix;
 template <> struct Mix<bf16_t> {
   typedef Mma<bf16_t> M;
-  static constexpr int PAD = 8, TILES = 2, PLANES = 2;
+  static constexpr int PAD = 16, TILES = 2, PLANES = 2;
   // in every block of 16 lanes, lane s gives the address of 4 columns of row s / 4 and gets column s of the four rows
   __device__ static __forceinline__ M::frag_t across(const bf16_t* tile, int ld, int step, int col, int lane) {
     const bf16_t* p = tile + (32 * step + 4 * (lane >> 4) + ((lane & 15) >> 2)) * ld + col + 4 * (lane & 3);
@@ -56,6 +56,13 @@ template <> struct Mix<float> {
     return make_float4(p[0], p[ld], p[2 * ld], p[3 * ld]);
   }
   __device__ static __forceinline__ void pack(const f32x4_t* p, M::frag_t (&o)[1]) { o[0] = make_float4(p[0][0], p[0][1], p[0][2], p[0][3]); }
+};
+
+// The state as an operand in LDS: 64 rows (its columns) of DK values. Piece p of row r lies at p ^ place: readers take a piece of 16 rows at once, and writers half a piece of 16 rows,
+// which padded rows would send to a quarter of the banks (a third of all LDS cycles).
+template <typename T, int DK> struct State {
+  static constexpr int PIECES = DK * (int)sizeof(T) / 16, W = 16 / (int)sizeof(T);
+  __device__ static __forceinline__ int at(int r, int p) { return r * DK + (p ^ (PIECES == 8 ? r >> 1 & 7 : r & 15)) * W; }
 };
 
 // b times the rows' weights, as N fragments whose sum it is: bf16 keeps 8 bits of the product in each, fp32 all of them
@@ -188,7 +195,7 @@ __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shar
     p.length = max(0, clamp_row(g.starts[n + 1], g.rows) - p.start);
     p.first = (int)min((long)(number - (p.start / g.segment + n)) * g.segment, (long)g.rows);
     p.segments = max(1, (p.length + g.segment - 1) / g.segment);
-    p.none |= p.first > 0 && p.first >= p.length;
+    p.none |= p.first < 0 || (p.first > 0 && p.first >= p.length);     // (starts that fall are found anywhere)
   }
   p.sequence = __builtin_amdgcn_readfirstlane(p.sequence);
   p.start = __builtin_amdgcn_readfirstlane(p.start);
@@ -212,13 +219,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
   typedef Mma<T> M;
   typedef Mix<T> X;
   typedef typename M::frag_t frag_t;
+  typedef State<T, DK> SL;
   constexpr int W = M::KV, LDA = DK + X::PAD, LDB = SLICE + X::PAD, STEPS = DK / M::KSTEP, OVER = 4 / X::TILES;
   constexpr int PA = CHUNK * DK / W / 256, PB = CHUNK * SLICE / W / 256;
   extern __shared__ __align__(16) unsigned char smem[];
   T* const at = reinterpret_cast<T*>(smem);                // [64][LDA]
   T* const bt = at + CHUNK * LDA;                          // [64][LDB]
-  T* const st = bt + CHUNK * LDB;                          // [SPLANES][64 columns of S][LDA]
-  __shared__ float power[CHUNK + 2];
+  T* const st = bt + CHUNK * LDB;                          // [PLANES][State]
+  __shared__ float pair_power[2 * CHUNK], row_power[2 * CHUNK];
   __shared__ int counted[4];
 
   const LinearJob job = g.job[blockIdx.y];
@@ -231,8 +239,47 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
   if (place.none || (SUM && place.segments == 1)) return;
   const int K = job.K, V = job.V, v0 = slice * SLICE;
 
+  // the rows of the walk: row r of the sequence is at base + r * step
+  const long sx = job.back ? -job.ld_x : job.ld_x, sa = job.back ? -job.ld_a : job.ld_a, sb = job.back ? -job.ld_b : job.ld_b;
+  const size_t origin = (size_t)place.start + (job.back ? (place.length ? place.length - 1 : 0) : 0);
+  const T* const bx = (const T*)job.x + origin * job.ld_x + (size_t)(head / job.share_x) * K + place.first * sx;
+  const T* const ba = (const T*)job.a + origin * job.ld_a + (size_t)(head / job.share_a) * K + place.first * sa;
+  const T* const bb = (const T*)job.b + origin * job.ld_b + (size_t)(head / job.share_b) * V + place.first * sb + v0;
+  const long out_step = job.back ? -job.ld_out : job.ld_out, out_at = (long)origin * job.ld_out + (long)head * V + place.first * out_step;
+  const int out_size = job.out_f32 ? 4 : (int)sizeof(T), tile = (blockIdx.x >> 8 & 1) ? 3 - wave : wave, row = 16 * tile + l16;
+
+  frag_t x[STEPS], ar[PA], br[PB];
+  Rows<T, VEC> rx, ra, rb;
+  auto request = [&](int r0) __attribute__((always_inline)) {
+    const int n = min(CHUNK, place.rows - r0);
+    ra.at(ba + r0 * sa, sa, n, K);
+#pragma unroll
+    for (int i = 0; i < PA; ++i) ar[i] = ra.get((tid + i * 256) / (DK / W), (tid + i * 256) % (DK / W) * W);
+    rb.at(bb + r0 * sb, sb, n, V - v0);
+#pragma unroll
+    for (int i = 0; i < PB; ++i) br[i] = rb.get((tid + i * 256) / (SLICE / W), (tid + i * 256) % (SLICE / W) * W);
+  };
+
+  // a wave's own rows are free for the next ones before the chunk ends
+  auto request_x = [&](int r0) __attribute__((always_inline)) {
+    rx.at(bx + r0 * sx, sx, min(CHUNK, place.rows - r0), K);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) x[s] = rx.get(row, s * M::KSTEP + l4 * W);
+  };
+  if (place.rows > 0) {
+    request(0);
+    if (!SUM) request_x(0);
+  }
+
+  // factors that every chunk shares, 0 from 64 on: intra g^(r-j) at 63 - r + j, update g^(n-1-j+late) at 64 - n + j, inter g^(r+1-late)
   const float lam = g.log_decay[head];
-  if (tid < CHUNK + 2) power[tid] = tid ? expf((float)tid * lam) : 1.f;
+  const auto power = [&](int n) __attribute__((always_inline)) { return n ? expf((float)n * lam) : 1.f; };
+  if (tid < 2 * CHUNK) {
+    const int n = CHUNK - 1 - tid;
+    pair_power[tid] = n < 0 ? 0.f : job.intra * power(n);
+    row_power[tid] = n < 0 ? 0.f : job.update * power(n + job.late);
+  }
+  const float into = job.inter * power(row + 1 - job.late), keep_whole = power(CHUNK);
 
   // S: this wave's 16 columns, all K rows
   f32x4_t S[DK / 16];
@@ -261,51 +308,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
 #pragma unroll
     for (int t = 0; t < DK / 16; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (!from || 16 * t + 4 * l4 + e >= K || col >= V) S[t][e] = 0.f;
+      for (int e = 0; e < 4; ++e) S[t][e] = from && 16 * t + 4 * l4 + e < K && col < V ? S[t][e] : 0.f;
   }
   __syncthreads();
-
-  // factors that every chunk shares: g^(r-j) of the pairs, g^(r+1-late) of the rows, g^(n-1-j+late) of the update of a whole chunk
-  const int row = 16 * wave + l16;
   float pairs[4][4], weight[16];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = 16 * t + 4 * l4 + e;
-      pairs[t][e] = j <= row ? job.intra * power[row - j] : 0.f;
-      weight[4 * t + e] = job.update * power[CHUNK - 1 - j + job.late];
-    }
-  const float into = job.inter * power[row + 1 - job.late];
-
-  // the rows of the walk: row r of the sequence is at base + r * step
-  const long sx = job.back ? -job.ld_x : job.ld_x, sa = job.back ? -job.ld_a : job.ld_a, sb = job.back ? -job.ld_b : job.ld_b;
-  const size_t origin = (size_t)place.start + (job.back ? (place.length ? place.length - 1 : 0) : 0);
-  const T* const bx = (const T*)job.x + origin * job.ld_x + (size_t)(head / job.share_x) * K + place.first * sx;
-  const T* const ba = (const T*)job.a + origin * job.ld_a + (size_t)(head / job.share_a) * K + place.first * sa;
-  const T* const bb = (const T*)job.b + origin * job.ld_b + (size_t)(head / job.share_b) * V + place.first * sb + v0;
-  const long out_step = job.back ? -job.ld_out : job.ld_out, out_at = (long)origin * job.ld_out + (long)head * V + place.first * out_step;
-  const int out_size = job.out_f32 ? 4 : (int)sizeof(T);
-
-  frag_t xr[STEPS], ar[PA], br[PB];
-  Rows<T, VEC> rx, ra, rb;
-  auto request = [&](int r0) __attribute__((always_inline)) {
-    const int n = min(CHUNK, place.rows - r0);
-    if (!SUM) {
-      rx.at(bx + r0 * sx, sx, n, K);
+    for (int e = 0; e < 4; ++e) pairs[t][e] = pair_power[CHUNK - 1 - row + 4 * l4 + 16 * t + e];
+  const auto weigh_rows = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) xr[s] = rx.get(row, s * M::KSTEP + l4 * W);
-    }
-    ra.at(ba + r0 * sa, sa, n, K);
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int i = 0; i < PA; ++i) ar[i] = ra.get((tid + i * 256) / (DK / W), (tid + i * 256) % (DK / W) * W);
-    rb.at(bb + r0 * sb, sb, n, V - v0);
-#pragma unroll
-    for (int i = 0; i < PB; ++i) br[i] = rb.get((tid + i * 256) / (SLICE / W), (tid + i * 256) % (SLICE / W) * W);
+      for (int e = 0; e < 4; ++e) weight[4 * t + e] = row_power[CHUNK - n + 4 * l4 + 16 * t + e];
   };
+  weigh_rows(CHUNK);
 
-  if (place.rows > 0) request(0);
   for (int r0 = 0; r0 < place.rows; r0 += CHUNK) {
     const int n = min(CHUNK, place.rows - r0);
     lds_barrier();
@@ -320,24 +338,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
       *reinterpret_cast<frag_t*>(bt + r * LDB + c) = rb.settle(br[i], r, c);
     }
     if (!SUM) {
-      T* const to = st + (16 * wave + l16) * LDA + 4 * l4;
 #pragma unroll
       for (int t = 0; t < DK / 16; ++t) {
         if constexpr (sizeof(T) == 2) {
+          T* const to = st + SL::at(16 * wave + l16, 2 * t + (l4 >> 1)) + 4 * (l4 & 1);
           uint2 h, l;
           X::split(S[t], h, l);
-          *reinterpret_cast<uint2*>(to + 16 * t) = h;
-          *reinterpret_cast<uint2*>(to + SLICE * LDA + 16 * t) = l;
+          *reinterpret_cast<uint2*>(to) = h;
+          *reinterpret_cast<uint2*>(to + SLICE * DK) = l;
         } else {
-          Store<float>::store4(reinterpret_cast<float*>(to) + 16 * t, S[t][0], S[t][1], S[t][2], S[t][3]);
+          Store<float>::store4(reinterpret_cast<float*>(st) + SL::at(16 * wave + l16, 4 * t + l4), S[t][0], S[t][1], S[t][2], S[t][3]);
         }
       }
     }
     lds_barrier();
-    frag_t x[STEPS];
     if (!SUM) {
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) x[s] = rx.settle(xr[s], row, s * M::KSTEP + l4 * W);
+      for (int s = 0; s < STEPS; ++s) x[s] = rx.settle(x[s], row, s * M::KSTEP + l4 * W);
     }
     if (r0 + CHUNK < place.rows) request(r0 + CHUNK);
     if (!SUM) {
@@ -348,9 +365,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
 #pragma unroll
       for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-        for (int p = 0; p < X::PLANES; ++p)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) o[t] = M::mma(M::load(st + (p * SLICE + 16 * t + l16) * LDA + s * M::KSTEP + l4 * W), x[s], o[t]);
+        for (int i = 0; i < 4 * X::PLANES; ++i) o[i & 3] = M::mma(M::load(st + SL::at(16 * i + l16, s * (M::KSTEP / W) + l4)), x[s], o[i & 3]);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -381,10 +396,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
             for (int t = 0; t < 4; ++t) o[t] = M::mma(b[t], of[p], o[t]);
         }
       };
-      if (wave == 0) mix(std::integral_constant<int, 1>());
-      else if (wave == 1) mix(std::integral_constant<int, 2>());
-      else if (wave == 2) mix(std::integral_constant<int, 3>());
+      if (tile == 0) mix(std::integral_constant<int, 1>());
+      else if (tile == 1) mix(std::integral_constant<int, 2>());
+      else if (tile == 2) mix(std::integral_constant<int, 3>());
       else mix(std::integral_constant<int, 4>());
+      if (r0 + CHUNK < place.rows) request_x(r0 + CHUNK);
       const int c = v0 + 4 * l4;
       if constexpr (VEC) {
         Rows<float, true> to;                              // (offsets in bytes; nothing is written where there is no result)
@@ -408,16 +424,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
       }
     }
     // the state after these rows
-    if (n < CHUNK) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int j = 16 * t + 4 * l4 + e;
-          weight[4 * t + e] = j < n ? job.update * power[n - 1 - j + job.late] : 0.f;
-        }
-    }
-    const float keep = power[n];
+    if (n < CHUNK) weigh_rows(n);
+    const float keep = n == CHUNK ? keep_whole : power(n);
 #pragma unroll
     for (int t = 0; t < DK / 16; ++t)
 #pragma unroll
@@ -592,7 +600,7 @@ __global__ __launch_bounds__(256) void step_kernel(LinearStepArgs a) {
 
 template <typename T, int DK, int PLANES, bool VEC, bool SUM> hipError_t walk_run(const LinearArgs& g, int jobs, hipStream_t s) {
   constexpr int LDA = DK + Mix<T>::PAD, LDB = SLICE + Mix<T>::PAD;
-  constexpr size_t lds = (size_t)(CHUNK * LDA + CHUNK * LDB + (SUM ? 0 : Mix<T>::PLANES * SLICE * LDA)) * sizeof(T);
+  constexpr size_t lds = (size_t)(CHUNK * LDA + CHUNK * LDB + (SUM ? 0 : Mix<T>::PLANES * SLICE * DK)) * sizeof(T);
   static const hipError_t allowed = hipFuncSetAttribute((const void*)walk_kernel<T, DK, PLANES, VEC, SUM>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (allowed != hipSuccess) return allowed;
   int slices = 0;
@@ -659,7 +667,6 @@ int linear_segment(int rows, int sequences, int walks, bool ragged) {
   const int average = rows / sequences;
   int segment = (int)((average + most - 1) / most);
   segment = (segment + CHUNK - 1) / CHUNK * CHUNK;
-  segment = segment < 256 ? 256 : segment;
   if (ragged && segment > 2048) segment = 2048;
   return length <= segment || (!ragged && most == 1) ? 0 : segment;
 }

@@ -203,6 +203,10 @@ def test_linear_starts_out_of_range_stay_inside():
         if lengths:
             assert off(o, reference(c)[0]) <= SUMS
     assert bool((o == 7.0).all())
+    c = mixing("f32", [700, 300], 1, 1, 16, 16)                # more than a segment, the starts falling
+    o, guard = c.space(1000, 16), c.ws()
+    c.op.forward(c.q, c.k, c.v, c.lam, o, starts=torch.tensor([1000, 40, 0], device="cuda", dtype=torch.int32), workspace=guard)
+    assert bool((o == 7.0).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
