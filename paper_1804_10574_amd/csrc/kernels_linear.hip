@@ -357,6 +357,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
       for (int s = 0; s < STEPS; ++s) x[s] = rx.settle(x[s], row, s * M::KSTEP + l4 * W);
     }
     if (r0 + CHUNK < place.rows) request(r0 + CHUNK);
+    // the state after these rows (before their results, which do not wait for it)
+    if (n < CHUNK) weigh_rows(n);
+    const float keep = n == CHUNK ? keep_whole : power(n);
+#pragma unroll
+    for (int t = 0; t < DK / 16; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[t][e] *= keep;
+#pragma unroll
+    for (int s = 0; s < OVER; ++s) {
+      frag_t w[PLANES];
+      weigh<PLANES>(X::across(bt, LDB, s, 16 * wave, lane), weight + 4 * X::TILES * s, w);
+#pragma unroll
+      for (int t = 0; t < DK / 16; t += 4) {
+        frag_t a[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = X::across(at, LDA, s, 16 * (t + i), lane);
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S[t + i] = M::mma(a[i], w[p], S[t + i]);
+      }
+    }
     if (!SUM) {
       // columns of the result, 16 at a time and four at once, so that no product waits for the one before: from the state
       f32x4_t o[4];
@@ -423,28 +445,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
             }
       }
     }
-    // the state after these rows
-    if (n < CHUNK) weigh_rows(n);
-    const float keep = n == CHUNK ? keep_whole : power(n);
-#pragma unroll
-    for (int t = 0; t < DK / 16; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) S[t][e] *= keep;
-#pragma unroll
-    for (int s = 0; s < OVER; ++s) {
-      frag_t w[PLANES];
-      weigh<PLANES>(X::across(bt, LDB, s, 16 * wave, lane), weight + 4 * X::TILES * s, w);
-#pragma unroll
-      for (int t = 0; t < DK / 16; t += 4) {
-        frag_t a[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = X::across(at, LDA, s, 16 * (t + i), lane);
-#pragma unroll
-        for (int p = 0; p < PLANES; ++p)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) S[t + i] = M::mma(a[i], w[p], S[t + i]);
-      }
-    }
   }
 
   float* to = nullptr;
@@ -465,9 +465,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
     }
 }
 
-// The states before each segment from the segments' own, in place, and the last one: a thread an element, segments in order
+// The states before each segment from the segments' own, in place, and the last one: a thread four elements (or one, where a state is no whole number of fours), segments
+// in order
+template <int E>
 __global__ __launch_bounds__(256) void scan_kernel(LinearArgs g, int blocks) {
-  const LinearJob& job = g.job[blockIdx.y];
+  typedef float vec_t __attribute__((ext_vector_type(E)));
+  const LinearJob job = g.job[blockIdx.y];
   const int K = job.K, V = job.V, pair = blockIdx.x / blocks, n = pair / g.heads, head = pair % g.heads;
   int start, length, first;
   if (g.starts) {
@@ -479,32 +482,38 @@ __global__ __launch_bounds__(256) void scan_kernel(LinearArgs g, int blocks) {
     first = n * max(1, (length + g.segment - 1) / g.segment);
   }
   const int count = (length + g.segment - 1) / g.segment;
-  const int i = (blockIdx.x - pair * blocks) * 256 + threadIdx.x;
+  const int i = ((blockIdx.x - pair * blocks) * 256 + threadIdx.x) * E;
   if (count < 2 || i >= K * V) return;                     // (the walk of a single segment has done all of it)
   const float lam = g.log_decay[head];
-  const int r = i / V, c = i - r * V;
   int slot = g.slots ? g.slots[n] : n;
   if ((unsigned)slot >= (unsigned)g.pool) slot = -1;
-  const size_t at = slot >= 0 ? ((size_t)slot * g.heads + head) * K * V + r * job.at_k + c * job.at_v : 0;
-  float s = job.state_in && slot >= 0 ? job.state_in[at] : 0.f;
-  const float keep = expf((float)g.segment * lam);
+  size_t at[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    const int r = (i + j) / V, c = i + j - r * V;
+    at[j] = slot >= 0 ? ((size_t)slot * g.heads + head) * K * V + r * job.at_k + c * job.at_v : 0;
+  }
+  vec_t s;
+#pragma unroll
+  for (int j = 0; j < E; ++j) s[j] = job.state_in && slot >= 0 ? job.state_in[at[j]] : 0.f;
+  const float keep = expf((float)g.segment * lam), keep_last = expf((float)(length - (count - 1) * g.segment) * lam);
   float* p = job.pieces + ((size_t)first * g.heads + head) * K * V + i;
   const size_t step = (size_t)g.heads * K * V;
   constexpr int AHEAD = 8;
   for (int k0 = 0; k0 < count; k0 += AHEAD) {
-    float own[AHEAD];
+    vec_t own[AHEAD];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) own[k] = p[(size_t)min(k0 + k, count - 1) * step];
+    for (int k = 0; k < AHEAD; ++k) own[k] = *reinterpret_cast<const vec_t*>(p + (size_t)min(k0 + k, count - 1) * step);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       if (k0 + k >= count) break;
-      p[(size_t)(k0 + k) * step] = s;
-      const bool last = k0 + k + 1 == count;
-      const int rows = length - (count - 1) * g.segment;
-      s = (last ? expf((float)rows * lam) : keep) * s + own[k];
+      *reinterpret_cast<vec_t*>(p + (size_t)(k0 + k) * step) = s;
+      s = (k0 + k + 1 == count ? keep_last : keep) * s + own[k];
     }
   }
-  if (job.state_out && slot >= 0) job.state_out[at] = s;
+  if (!job.state_out || slot < 0) return;
+#pragma unroll
+  for (int j = 0; j < E; ++j) job.state_out[at[j]] = s[j];
 }
 
 // Sums over the heads that share keys and values
@@ -637,9 +646,15 @@ template <typename T> hipError_t walk_typed(const LinearArgs& g, int jobs, hipSt
     hipError_t e = vec ? walk_any<T, true, true>(g, jobs, s) : walk_any<T, false, true>(g, jobs, s);
     if (e != hipSuccess) return e;
     int most = 0;
-    for (int i = 0; i < jobs; ++i) most = g.job[i].K * g.job[i].V > most ? g.job[i].K * g.job[i].V : most;
-    const int blocks = (most + 255) / 256;
-    DDG_LAUNCH(scan_kernel, dim3(blocks * g.sequences * g.heads, jobs), dim3(256), 0, s, g, blocks);
+    bool fours = true;
+    for (int i = 0; i < jobs; ++i) {
+      const int cells = g.job[i].K * g.job[i].V;
+      most = cells > most ? cells : most;
+      fours &= cells % 4 == 0;
+    }
+    const int each = fours ? 1024 : 256, blocks = (most + each - 1) / each;
+    if (fours) DDG_LAUNCH(scan_kernel<4>, dim3(blocks * g.sequences * g.heads, jobs), dim3(256), 0, s, g, blocks);
+    else DDG_LAUNCH(scan_kernel<1>, dim3(blocks * g.sequences * g.heads, jobs), dim3(256), 0, s, g, blocks);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
