@@ -86,7 +86,7 @@ struct Cut { int segment; long segments; size_t pieces; };
 Cut cut_of(const ddg_linear_desc& d, bool backward, bool ragged) {
   const long k = slices_of(d.dim_k), v = slices_of(d.dim_v), walks = d.heads * (backward ? 2 * k + v : v);
   Cut c;
-  c.segment = linear_segment(d.rows, d.sequences, (int)(walks < (1 << 30) ? walks : 1 << 30), ragged);
+  c.segment = linear_segment(d.rows, d.sequences, (int)(walks < (1 << 30) ? walks : 1 << 30), ragged, d.dtype);
   c.segments = !c.segment ? d.sequences : ragged ? d.rows / c.segment + (long)d.sequences : (long)d.sequences * ((d.rows / d.sequences + c.segment - 1) / c.segment);
   c.pieces = c.segment ? (size_t)c.segments * d.heads * d.dim_k * d.dim_v * 4 : 0;
   c.pieces = (c.pieces + 255) / 256 * 256;
@@ -342,10 +342,14 @@ ddg_status ddg_linear_attention_backward(const ddg_linear_desc* desc, const void
   for (int i = 0; i < jobs; ++i) a.job[i].slices = (int)slices_of(a.job[i].V);
   const hipStream_t s = (hipStream_t)d.stream;
   hipError_t e = linear_launch(a, jobs, s);
-  if (e == hipSuccess && share > 1 && dk && d.rows)
-    e = linear_share_launch(dk_heads, dk, d.ld_k, starts, d.sequences, d.rows, d.kv_heads, share, d.dim_k, d.dtype, s);
-  if (e == hipSuccess && share > 1 && dv && d.rows)
-    e = linear_share_launch(dv_heads, dv, d.ld_v, starts, d.sequences, d.rows, d.kv_heads, share, d.dim_v, d.dtype, s);
+  if (e == hipSuccess && share > 1 && d.rows && (dk || dv)) {
+    LinearShareArgs sum{};
+    sum.starts = starts; sum.sequences = d.sequences; sum.rows = d.rows; sum.groups = d.kv_heads; sum.share = share; sum.dtype = d.dtype;
+    int count = 0;
+    if (dk) sum.of[count++] = {dk_heads, dk, d.ld_k, d.dim_k};
+    if (dv) sum.of[count++] = {dv_heads, dv, d.ld_v, d.dim_v};
+    e = linear_share_launch(sum, count, s);
+  }
   return done(e, "linear attention backward");
 }
 

@@ -56,10 +56,15 @@ struct LinearStepArgs {
   float scale;
 };
 constexpr int LINEAR_DIM_MAX = 256;
-int linear_segment(int rows, int sequences, int walks, bool ragged);   // rows of a segment; 0: sequences are not split
+int linear_segment(int rows, int sequences, int walks, bool ragged, int dtype);   // rows of a segment; 0: sequences are not split
 hipError_t linear_launch(const LinearArgs& a, int jobs, hipStream_t s);
 hipError_t linear_step_launch(const LinearStepArgs& a, hipStream_t s);
-// out [rows][groups][cols] = sums of `share` neighbouring heads of in [rows][groups * share][cols], fp32, in order
-hipError_t linear_share_launch(const float* in, void* out, long ld_out, const int* starts, int sequences, int rows, int groups, int share, int cols, int dtype, hipStream_t s);
+// out [rows][groups][cols] = sums of `share` neighbouring heads of in [rows][groups * share][cols], fp32, in order; up to two of them
+struct LinearShareArgs {
+  struct One { const float* in; void* out; long ld; int cols; } of[2];
+  const int* starts;
+  int sequences, rows, groups, share, dtype;
+};
+hipError_t linear_share_launch(const LinearShareArgs& a, int count, hipStream_t s);
 
 }  // namespace ddg

@@ -104,6 +104,52 @@ template <int U, int TPR> __device__ __forceinline__ void load_gain(const float*
     }
 }
 
+// 8 columns of a row from column c on, zeros behind the row's end, without a conditional load (where branches meet, the compiler waits for all loads in flight): what lies past
+// the end is read from the row's last 8 columns and moved into place when it is needed.
+template <typename T, bool VEC> struct Row8 {
+  Unit<T, VEC> v;
+  int past;                                                // columns that were read before c; 8: nothing is there
+  __device__ __forceinline__ void load(const T* row, int c, int cols) {
+    const int from = VEC || cols >= 8 ? min(c, cols - 8) : 0;
+    past = min(c - from, 8);
+    if (VEC || cols >= 8) {
+      v.load(row + from, 8);
+    } else {
+      T e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = row[min(i, cols - 1)];
+      __builtin_memcpy(&v, e, sizeof(e));
+      if (c == 0) past = cols - 8;                         // (fewer than 8 columns: those from `cols` on are not there)
+    }
+  }
+  __device__ __forceinline__ void zero() { v.zero(); past = 0; }
+  __device__ __forceinline__ void get(float (&o)[8]) const {
+    v.get(o);
+    if (VEC) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = past ? 0.f : o[i];
+    } else {
+#pragma unroll
+      for (int k = 4; k; k >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = past > 0 && (past & k) ? (i + k < 8 ? o[i + k] : 0.f) : o[i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = past == 8 || (past < 0 && i >= 8 + past) ? 0.f : o[i];
+    }
+  }
+};
+// The same of fp32 [cols], `fill` where there is none
+__device__ __forceinline__ void columns8(const float* p, int c, int cols, float fill, float (&o)[8]) {
+  if (!p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = fill;
+    return;
+  }
+  Row8<float, false> r;                                    // (vectors may lie anywhere)
+  r.load(p, c, cols);
+  r.get(o);
+}
+
 inline bool aligned(const void* p, long ld, size_t size, size_t to) { return !p || ((uintptr_t)p % to == 0 && (size_t)ld * size % to == 0); }
 
 }  // namespace

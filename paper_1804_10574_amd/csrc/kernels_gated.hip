@@ -43,16 +43,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
   const int shift = a.group ? __builtin_ctz(lanes) : 0;
   const bool wide = a.mode >= GATE_PLAIN;
   int row = blockIdx.x * RPB + threadIdx.x / TPR;
-  Unit<T, VEC> yv[U], rv[U], gv[U];
+  Row8<T, VEC> yv[U], rv[U], gv[U];
   auto request = [&](int r) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = lane + i * TPR, n = a.cols - u * 8;
-      if (u < upr) {
-        yv[i].load((const T*)a.y + (size_t)r * a.ld_y + u * 8, n);
-        if (wide) gv[i].load((const T*)a.gate + (size_t)r * a.ld_gate + u * 8, n);
-        if (a.residual) rv[i].load((const T*)a.residual + (size_t)r * a.ld_residual + u * 8, n);
-      }
+      const int c = (lane + i * TPR) * 8;
+      yv[i].load((const T*)a.y + (size_t)r * a.ld_y, c, a.cols);
+      if (wide) gv[i].load((const T*)a.gate + (size_t)r * a.ld_gate, c, a.cols);
+      if (a.residual) rv[i].load((const T*)a.residual + (size_t)r * a.ld_residual, c, a.cols);
     }
   };
 #pragma unroll
@@ -60,9 +58,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
   if (AHEAD && row < a.rows) request(row);
   float gy[U][8], gx[U][8], gc[U][8];
   if (AHEAD) {
-    load_gain<U, TPR>(a.gain_y, lane, a.cols, gy);
-    load_gain<U, TPR>(a.gain_x, lane, a.cols, gx);
-    load_gain<U, TPR>(a.mode == GATE_COLUMN ? (const float*)a.gate : nullptr, lane, a.cols, gc);
+#pragma unroll
+    for (int i = 0; i < U; ++i) columns8(a.gain_y, (lane + i * TPR) * 8, a.cols, 1.f, gy[i]);
+#pragma unroll
+    for (int i = 0; i < U; ++i) columns8(a.gain_x, (lane + i * TPR) * 8, a.cols, 1.f, gx[i]);
+#pragma unroll
+    for (int i = 0; i < U; ++i) columns8(a.mode == GATE_COLUMN ? (const float*)a.gate : nullptr, (lane + i * TPR) * 8, a.cols, 1.f, gc[i]);
   }
   const float inv = 1.f / (float)a.cols, inv_group = a.group ? 1.f / (float)a.group : inv;
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
@@ -91,8 +92,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
         if (a.rstd_y && u < upr && (u & (lanes - 1)) == 0) a.rstd_y[(size_t)row * (upr >> shift) + (u >> shift)] = rstd;
       }
       if (!AHEAD) {
-        load_gain<1, TPR>(a.gain_y, u, a.cols, reinterpret_cast<float(&)[1][8]>(gy[i]));
-        load_gain<1, TPR>(a.mode == GATE_COLUMN ? (const float*)a.gate : nullptr, u, a.cols, reinterpret_cast<float(&)[1][8]>(gc[i]));
+        columns8(a.gain_y, u * 8, a.cols, 1.f, gy[i]);
+        columns8(a.mode == GATE_COLUMN ? (const float*)a.gate : nullptr, u * 8, a.cols, 1.f, gc[i]);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = lane + i * TPR, n = a.cols - u * 8;
-      if (!AHEAD) load_gain<1, TPR>(a.gain_x, u, a.cols, reinterpret_cast<float(&)[1][8]>(gx[i]));
+      if (!AHEAD) columns8(a.gain_x, u * 8, a.cols, 1.f, gx[i]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[i][j] = x[i][j] * rstd * gx[i][j];
       if (u < upr) Unit<T, VEC>::store((T*)a.out + (size_t)row * a.ld_out + u * 8, x[i], n);
@@ -129,22 +130,20 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
   const int lane = threadIdx.x % TPR, part = threadIdx.x / TPR, step = gridDim.x * RPB;
   const int upr = (a.cols + 7) / 8, lanes = a.group / 8, shift = a.group ? __builtin_ctz(lanes) : 0, per_row = a.group ? upr >> shift : 1;
   const bool wide = a.mode >= GATE_PLAIN, column = a.mode == GATE_COLUMN;
-  Unit<T, VEC> xv[U], yv[U], gv[U], dv[U], sv[U];
+  Row8<T, VEC> xv[U], yv[U], gv[U], dv[U], sv[U];
   float ry[U], rx = 0.f;
   auto request = [&](int r) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = lane + i * TPR, n = a.cols - u * 8;
-      if (u < upr) {
-        yv[i].load((const T*)a.y + (size_t)r * a.ld_y + u * 8, n);
-        if (wide) gv[i].load((const T*)a.gate + (size_t)r * a.ld_gate + u * 8, n);
-        if (a.d_out) {
-          xv[i].load((const T*)a.x + (size_t)r * a.ld_x + u * 8, n);
-          dv[i].load((const T*)a.d_out + (size_t)r * a.ld_out + u * 8, n);
-        }
-        if (a.d_x) sv[i].load((const T*)a.d_x + (size_t)r * a.ld_x + u * 8, n);
-        ry[i] = a.rstd_y[(size_t)r * per_row + (a.group ? u >> shift : 0)];
+      const int u = lane + i * TPR, c = u * 8;
+      yv[i].load((const T*)a.y + (size_t)r * a.ld_y, c, a.cols);
+      if (wide) gv[i].load((const T*)a.gate + (size_t)r * a.ld_gate, c, a.cols);
+      if (a.d_out) {
+        xv[i].load((const T*)a.x + (size_t)r * a.ld_x, c, a.cols);
+        dv[i].load((const T*)a.d_out + (size_t)r * a.ld_out, c, a.cols);
       }
+      if (a.d_x) sv[i].load((const T*)a.d_x + (size_t)r * a.ld_x, c, a.cols);
+      ry[i] = a.rstd_y[(size_t)r * per_row + (a.group ? min(u >> shift, per_row - 1) : 0)];
     }
     if (a.d_out) rx = a.rstd_x[r];
   };
@@ -158,9 +157,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
   int row = blockIdx.x * RPB + part;
   if (AHEAD && row < a.rows) request(row);
   if (AHEAD) {
-    load_gain<U, TPR>(a.gain_y, lane, a.cols, gy);
-    load_gain<U, TPR>(a.gain_x, lane, a.cols, gx);
-    load_gain<U, TPR>(column ? (const float*)a.gate : nullptr, lane, a.cols, gc);
+#pragma unroll
+    for (int i = 0; i < U; ++i) columns8(a.gain_y, (lane + i * TPR) * 8, a.cols, 1.f, gy[i]);
+#pragma unroll
+    for (int i = 0; i < U; ++i) columns8(a.gain_x, (lane + i * TPR) * 8, a.cols, 1.f, gx[i]);
+#pragma unroll
+    for (int i = 0; i < U; ++i) columns8(column ? (const float*)a.gate : nullptr, (lane + i * TPR) * 8, a.cols, 1.f, gc[i]);
   }
   const float inv = 1.f / (float)a.cols, inv_group = a.group ? 1.f / (float)a.group : inv;
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
@@ -173,9 +175,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
       xv[i].get(x[i]); dv[i].get(d[i]); yv[i].get(y[i]); gv[i].get(g[i]); sv[i].get(s[i]);
       by[i] = ry[i];
       if (!AHEAD) {
-        load_gain<1, TPR>(a.gain_y, u, a.cols, reinterpret_cast<float(&)[1][8]>(gy[i]));
-        load_gain<1, TPR>(a.gain_x, u, a.cols, reinterpret_cast<float(&)[1][8]>(gx[i]));
-        load_gain<1, TPR>(column ? (const float*)a.gate : nullptr, u, a.cols, reinterpret_cast<float(&)[1][8]>(gc[i]));
+        columns8(a.gain_y, u * 8, a.cols, 1.f, gy[i]);
+        columns8(a.gain_x, u * 8, a.cols, 1.f, gx[i]);
+        columns8(column ? (const float*)a.gate : nullptr, u * 8, a.cols, 1.f, gc[i]);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {

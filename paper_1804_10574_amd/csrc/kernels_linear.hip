@@ -62,7 +62,8 @@ template <> struct Mix<float> {
 // which padded rows would send to a quarter of the banks (a third of all LDS cycles).
 template <typename T, int DK> struct State {
   static constexpr int PIECES = DK * (int)sizeof(T) / 16, W = 16 / (int)sizeof(T);
-  __device__ static __forceinline__ int at(int r, int p) { return r * DK + (p ^ (PIECES == 8 ? r >> 1 & 7 : r & 15)) * W; }
+  static constexpr int PLACES = PIECES % 16 == 0 ? 16 : PIECES % 8 == 0 ? 8 : 4, ROWS = PIECES < 16 && PIECES % 12 ? 16 / PIECES : 1;     // (rows in 256 bytes)
+  __device__ static __forceinline__ int at(int r, int p) { return r * DK + (p ^ (r / ROWS & (PLACES - 1))) * W; }
 };
 
 // b times the rows' weights, as N fragments whose sum it is: bf16 keeps 8 bits of the product in each, fp32 all of them
@@ -179,20 +180,28 @@ __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shar
     p.segments = 1;
     p.none = false;
   } else {
-    int before = 0;
+    int before = 0, start = 0, end = 0;
     for (int n0 = 0; n0 < g.sequences; n0 += 256) {
-      const int n = n0 + threadIdx.x;
-      const bool is = n < g.sequences && clamp_row(g.starts[n < g.sequences ? n : 0], g.rows) / g.segment + n <= number;
-      before += __popcll(__ballot(is));
+      const int n = min(n0 + (int)threadIdx.x, g.sequences - 1), s0 = clamp_row(g.starts[n], g.rows), s1 = clamp_row(g.starts[n + 1], g.rows);
+      const bool is = n == n0 + (int)threadIdx.x && s0 / g.segment + n <= number;
+      const int here = __popcll(__ballot(is));
+      before += here;
+      if (here) {                                          // the last one that begins at or before this number, in this wave
+        start = __shfl(s0, here - 1);
+        end = __shfl(s1, here - 1);
+      }
     }
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = before;
+    if ((threadIdx.x & 63) == 0) {
+      const int w = threadIdx.x >> 6;
+      shared[3 * w] = before; shared[3 * w + 1] = start; shared[3 * w + 2] = end;
+    }
     __syncthreads();
-    before = shared[0] + shared[1] + shared[2] + shared[3];
+    before = shared[0] + shared[3] + shared[6] + shared[9];
     p.sequence = before - 1;
     p.none = before < 1;
-    const int n = max(0, p.sequence);
-    p.start = clamp_row(g.starts[n], g.rows);
-    p.length = max(0, clamp_row(g.starts[n + 1], g.rows) - p.start);
+    const int n = max(0, p.sequence), w = n >> 6 & 3;
+    p.start = shared[3 * w + 1];
+    p.length = max(0, shared[3 * w + 2] - p.start);
     p.first = (int)min((long)(number - (p.start / g.segment + n)) * g.segment, (long)g.rows);
     p.segments = max(1, (p.length + g.segment - 1) / g.segment);
     p.none |= p.first < 0 || (p.first > 0 && p.first >= p.length);     // (starts that fall are found anywhere)
@@ -215,19 +224,19 @@ __device__ __forceinline__ int on_die(int id, int total) {
 
 // SUM: only the state of the segment's own rows, for the scan. PLANES: fragments a weighted b is taken apart into.
 template <typename T, int DK, int PLANES, bool VEC, bool SUM>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk_kernel(LinearArgs g) {
+__global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 2 : 1) void walk_kernel(LinearArgs g) {
   typedef Mma<T> M;
   typedef Mix<T> X;
   typedef typename M::frag_t frag_t;
   typedef State<T, DK> SL;
-  constexpr int W = M::KV, LDA = DK + X::PAD, LDB = SLICE + X::PAD, STEPS = DK / M::KSTEP, OVER = 4 / X::TILES;
+  constexpr int W = M::KV, LDA = DK + X::PAD, LDB = SLICE + X::PAD, STEPS = DK / M::KSTEP, OVER = 4 / X::TILES, GROUP = DK % 64 ? 2 : 4;
   constexpr int PA = CHUNK * DK / W / 256, PB = CHUNK * SLICE / W / 256;
   extern __shared__ __align__(16) unsigned char smem[];
   T* const at = reinterpret_cast<T*>(smem);                // [64][LDA]
   T* const bt = at + CHUNK * LDA;                          // [64][LDB]
   T* const st = bt + CHUNK * LDB;                          // [PLANES][State]
   __shared__ float pair_power[2 * CHUNK], row_power[2 * CHUNK];
-  __shared__ int counted[4];
+  __shared__ int counted[12];
 
   const LinearJob job = g.job[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
@@ -369,14 +378,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DK <= 128 ? 2 : 1) void walk
       frag_t w[PLANES];
       weigh<PLANES>(X::across(bt, LDB, s, 16 * wave, lane), weight + 4 * X::TILES * s, w);
 #pragma unroll
-      for (int t = 0; t < DK / 16; t += 4) {
-        frag_t a[4];
+      for (int t = 0; t < DK / 16; t += GROUP) {
+        frag_t a[GROUP];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = X::across(at, LDA, s, 16 * (t + i), lane);
+        for (int i = 0; i < GROUP; ++i) a[i] = X::across(at, LDA, s, 16 * (t + i), lane);
 #pragma unroll
         for (int p = 0; p < PLANES; ++p)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) S[t + i] = M::mma(a[i], w[p], S[t + i]);
+          for (int i = 0; i < GROUP; ++i) S[t + i] = M::mma(a[i], w[p], S[t + i]);
       }
     }
     if (!SUM) {
@@ -516,16 +525,17 @@ __global__ __launch_bounds__(256) void scan_kernel(LinearArgs g, int blocks) {
   for (int j = 0; j < E; ++j) job.state_out[at[j]] = s[j];
 }
 
-// Sums over the heads that share keys and values
-template <typename T> __global__ __launch_bounds__(256) void share_kernel(const float* in, T* out, long ld_out, const int* starts, int sequences, int rows, int groups, int share, int cols) {
+// Sums over the heads that share keys and values: a workgroup a row, of the keys' gradients or of the values'
+template <typename T> __global__ __launch_bounds__(256) void share_kernel(LinearShareArgs a) {
+  const LinearShareArgs::One one = a.of[blockIdx.y];
   const int r = blockIdx.x;
-  if (starts && (r < starts[0] || r >= starts[sequences])) return;
-  const float* p = in + (size_t)r * groups * share * cols;
-  for (int i = threadIdx.x; i < groups * cols; i += 256) {
-    const int h = i / cols, c = i - h * cols;
+  if (a.starts && (r < a.starts[0] || r >= a.starts[a.sequences])) return;
+  const float* p = one.in + (size_t)r * a.groups * a.share * one.cols;
+  for (int i = threadIdx.x; i < a.groups * one.cols; i += 256) {
+    const int h = i / one.cols, c = i - h * one.cols;
     float t = 0.f;
-    for (int k = 0; k < share; ++k) t += p[(size_t)(h * share + k) * cols + c];
-    Store<T>::store1(out + (size_t)r * ld_out + i, t);
+    for (int k = 0; k < a.share; ++k) t += p[(size_t)(h * a.share + k) * one.cols + c];
+    Store<T>::store1((T*)one.out + (size_t)r * one.ld + i, t);
   }
 }
 
@@ -629,7 +639,12 @@ template <typename T, int DK, bool VEC, bool SUM> hipError_t walk_planes(const L
 template <typename T, bool VEC, bool SUM> hipError_t walk_any(const LinearArgs& g, int jobs, hipStream_t s) {
   int most = 0;
   for (int j = 0; j < jobs; ++j) most = g.job[j].K > most ? g.job[j].K : most;
-  return most <= 64 ? walk_planes<T, 64, VEC, SUM>(g, jobs, s) : most <= 128 ? walk_planes<T, 128, VEC, SUM>(g, jobs, s) : walk_planes<T, 256, VEC, SUM>(g, jobs, s);
+  if (most <= 32) return walk_planes<T, 32, VEC, SUM>(g, jobs, s);
+  if (most <= 64) return walk_planes<T, 64, VEC, SUM>(g, jobs, s);
+  if (most <= 96) return walk_planes<T, 96, VEC, SUM>(g, jobs, s);
+  if (most <= 128) return walk_planes<T, 128, VEC, SUM>(g, jobs, s);
+  if (most <= 192) return walk_planes<T, 192, VEC, SUM>(g, jobs, s);
+  return walk_planes<T, 256, VEC, SUM>(g, jobs, s);
 }
 // Pieces of 16 bytes, and a chunk of rows inside the 31 bits of an offset
 bool whole(const void* p, long ld, int dim, size_t size) {
@@ -675,13 +690,14 @@ template <typename T> hipError_t step_typed(const LinearStepArgs& a, hipStream_t
 
 }  // namespace
 
-// Two workgroups a compute unit are resident: fewer walks than that are cut. Ragged sequences: nobody knows how long the longest is, and one of all the rows is allowed for.
-int linear_segment(int rows, int sequences, int walks, bool ragged) {
-  const int length = ragged ? rows : rows / sequences;
-  const long have = (long)sequences * walks, most = have < 512 ? (512 + have - 1) / have : 1;     // segments a sequence of average length
-  const int average = rows / sequences;
-  int segment = (int)((average + most - 1) / most);
-  segment = (segment + CHUNK - 1) / CHUNK * CHUNK;
+// Two workgroups a compute unit are resident: fewer walks than that are cut, for as many (a prompt of 16384 rows, 16 heads of 128, bf16: 130 us in segments of 1024 rows, 140 of 512, 172
+// of 2048). A segment costs three passes over a state, so the shortest is three chunks (3010 ragged rows of 12 heads, 64 x 128: 35 us, 39 with two chunks, 44 with one; 58 uncut), of fp32,
+// whose chunks take longer, one (777 ragged rows, gradients: 67 us, 70 with two, 130 uncut). Nobody knows how long the longest of ragged sequences is: 2048 rows are the most.
+int linear_segment(int rows, int sequences, int walks, bool ragged, int dtype) {
+  const int length = ragged ? rows : rows / sequences, average = rows / sequences, least = dtype == BF16 ? 3 * CHUNK : CHUNK;
+  const long have = (long)sequences * walks, most = have < 512 ? (512 + have - 1) / have : 1;     // segments of a sequence of average length
+  int segment = ((int)((average + most - 1) / most) + CHUNK - 1) / CHUNK * CHUNK;
+  segment = segment < least ? least : segment;
   if (ragged && segment > 2048) segment = 2048;
   return length <= segment || (!ragged && most == 1) ? 0 : segment;
 }
@@ -690,10 +706,9 @@ hipError_t linear_launch(const LinearArgs& a, int jobs, hipStream_t s) { return 
 
 hipError_t linear_step_launch(const LinearStepArgs& a, hipStream_t s) { return a.dtype == BF16 ? step_typed<bf16_t>(a, s) : step_typed<float>(a, s); }
 
-hipError_t linear_share_launch(const float* in, void* out, long ld_out, const int* starts, int sequences, int rows, int groups, int share, int cols, int dtype,
-                               hipStream_t s) {
-  if (dtype == BF16) DDG_LAUNCH(share_kernel<bf16_t>, dim3(rows), dim3(256), 0, s, in, (bf16_t*)out, ld_out, starts, sequences, rows, groups, share, cols);
-  else DDG_LAUNCH(share_kernel<float>, dim3(rows), dim3(256), 0, s, in, (float*)out, ld_out, starts, sequences, rows, groups, share, cols);
+hipError_t linear_share_launch(const LinearShareArgs& a, int count, hipStream_t s) {
+  if (a.dtype == BF16) DDG_LAUNCH(share_kernel<bf16_t>, dim3(a.rows, count), dim3(256), 0, s, a);
+  else DDG_LAUNCH(share_kernel<float>, dim3(a.rows, count), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

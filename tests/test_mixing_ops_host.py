@@ -121,7 +121,7 @@ def test_linear_refusals():
 
 
 def test_linear_workspace():
-    short = lin(rows=256)
+    short = lin(rows=192)
     assert short.workspace_bytes() == 0 and short.workspace_bytes(True) == 0
     long = lin(rows=1 << 16)
     need, both = long.workspace_bytes(), long.workspace_bytes(True)
@@ -137,7 +137,7 @@ def test_linear_workspace():
     assert shared.workspace_bytes() == 0 and shared.workspace_bytes(True) >= 100 * 4 * (32 + 48) * 4
     refused(INVALID, "workspace of", shared.backward, A, B, C_, D, E, F, G, H)
     shared.backward(A, B, C_, D, E, F, G, H, workspace=Space(shared.workspace_bytes(True)))
-    assert max(need, both) < 3.1 * 4 * 32 * 48 * 4 * (1 << 16) / 256 + 4096   # pieces: at most one per 256 rows
+    assert max(need, both) < 3.1 * 4 * 32 * 48 * 4 * (1 << 16) / 192 + 4096   # pieces: at most one per 192 rows
 
 
 def test_linear_backward_refusals():
