@@ -467,7 +467,7 @@ ddg_status ddg_linear_attention_step(const ddg_linear_desc* d, const void* q, co
  * rstd = (mean of squares + eps)^(-1/2), of y over `group` neighbouring columns (0: the row), of x over the row. gate: DDG_GATE_NONE (factor 1), _COLUMN (fp32 [cols], a
  * learned factor of each column), or [rows][cols] as it is (_PLAIN), through 1 / (1 + exp(-gate)) (_SIGMOID), or times that (_SILU). residual NULL: 0. gain_y, gain_x:
  * fp32 [cols], NULL: 1. x_out, out, rstd_y (fp32 [rows][cols / group], or [rows]), rstd_x (fp32 [rows]): each may be NULL. x_out may be y or residual (same
- * ld). Sums are fp32, out comes from the unrounded x. At most 16384 columns. */
+ * ld). Sums are fp32, out comes from the unrounded x. At most 8192 columns. */
 enum { DDG_GATE_NONE = 0, DDG_GATE_COLUMN = 1, DDG_GATE_PLAIN = 2, DDG_GATE_SIGMOID = 3, DDG_GATE_SILU = 4 };
 typedef struct {
   int rows, cols, dtype;

@@ -187,7 +187,7 @@ ddg_status ddg_gated_join(const ddg_gated_join_desc* desc, const void* y, const 
 size_t ddg_gated_join_workspace(const ddg_gated_join_desc* desc) {
   ddg_gated_join_desc d;
   GatedArgs a;
-  return gated_desc(desc, &d, &a) == DDG_OK ? (size_t)gated_groups(d.rows, d.cols) * d.cols * 4 * (d.gate == GATE_COLUMN ? 3 : 2) : 0;
+  return gated_desc(desc, &d, &a) == DDG_OK ? (size_t)gated_groups(d.rows, d.cols) * ((d.cols + 7) / 8 * 8) * 4 * (d.gate == GATE_COLUMN ? 3 : 2) : 0;
 }
 
 ddg_status ddg_gated_join_backward(const ddg_gated_join_desc* desc, const void* y, const float* rstd_y, const void* gate, const void* x, const float* rstd_x,

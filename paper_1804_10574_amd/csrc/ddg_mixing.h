@@ -20,12 +20,12 @@ struct GatedArgs {
   const void* y; const void* gate; const void* residual; const float* gain_y; const float* gain_x;   // gate: [rows][cols], or fp32 [cols] (GATE_COLUMN)
   void* x; void* out; float* rstd_y; float* rstd_x;             // forward: results; backward: x and both rstd are operands
   const void* d_out; const void* d_x;
-  void* d_residual; void* d_y; void* d_gate; float* d_gain_y; float* d_gain_x; float* partial;   // partial: [3][gated_groups][cols]
+  void* d_residual; void* d_y; void* d_gate; float* d_gain_y; float* d_gain_x; float* partial;   // partial: [3][gated_groups][cols in whole eights]
   long ld_y, ld_gate, ld_residual, ld_x, ld_out;
   int rows, cols, dtype, group, mode;
   float eps, scale, residual_scale;
 };
-constexpr int GATED_COLS_MAX = 16384;
+constexpr int GATED_COLS_MAX = 8192;
 int gated_groups(int rows, int cols);        // workgroups of the backward launch, each with rows of partial sums
 hipError_t gated_forward_launch(const GatedArgs& a, hipStream_t s);
 hipError_t gated_backward_launch(const GatedArgs& a, hipStream_t s);

@@ -11,8 +11,9 @@
 namespace ddg {
 namespace {
 
-// Rows of two units a lane leave no registers for the next row's operands
-template <int W, int U> constexpr bool AHEAD_FITS = U == 1;
+// A unit of 8 columns a lane. 16 waves have 128 registers a lane, which leaves none for the next row's operands (4096 x 8192 in bf16, backward: 116 us; 8 waves of two units, whose
+// registers do not fit, 177).
+constexpr int U = 1;
 
 // Sum over the `lanes` (a power of two) neighbouring lanes that share a norm, in each of them
 __device__ __forceinline__ float lanes_sum(float v, int lanes) {
@@ -34,14 +35,15 @@ __device__ __forceinline__ float gate_of(int mode, float g, float& slope) {
   return g * sig;
 }
 
-template <typename T, int W, int U, bool VEC>
+// COLUMN: the gate is a factor of each column, else a tensor or nothing
+template <typename T, int W, bool VEC, bool COLUMN>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(GatedArgs a) {
   constexpr int TPR = W * 64, RPB = W == 1 ? 4 : 1;
-  constexpr bool AHEAD = AHEAD_FITS<W, U>;
+  constexpr bool AHEAD = W < 16;
   __shared__ float red[2][2][W];
   const int lane = threadIdx.x % TPR, upr = (a.cols + 7) / 8, step = gridDim.x * RPB, lanes = a.group / 8;
   const int shift = a.group ? __builtin_ctz(lanes) : 0;
-  const bool wide = a.mode >= GATE_PLAIN;
+  const bool wide = !COLUMN && a.mode >= GATE_PLAIN;
   int row = blockIdx.x * RPB + threadIdx.x / TPR;
   Row8<T, VEC> yv[U], rv[U], gv[U];
   auto request = [&](int r) __attribute__((always_inline)) {
@@ -57,13 +59,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
   for (int i = 0; i < U; ++i) { yv[i].zero(); rv[i].zero(); gv[i].zero(); }
   if (AHEAD && row < a.rows) request(row);
   float gy[U][8], gx[U][8], gc[U][8];
-  if (AHEAD) {
+  {
 #pragma unroll
     for (int i = 0; i < U; ++i) columns8(a.gain_y, (lane + i * TPR) * 8, a.cols, 1.f, gy[i]);
 #pragma unroll
     for (int i = 0; i < U; ++i) columns8(a.gain_x, (lane + i * TPR) * 8, a.cols, 1.f, gx[i]);
 #pragma unroll
-    for (int i = 0; i < U; ++i) columns8(a.mode == GATE_COLUMN ? (const float*)a.gate : nullptr, (lane + i * TPR) * 8, a.cols, 1.f, gc[i]);
+    for (int i = 0; i < U; ++i) columns8(COLUMN ? (const float*)a.gate : nullptr, (lane + i * TPR) * 8, a.cols, 1.f, gc[i]);
   }
   const float inv = 1.f / (float)a.cols, inv_group = a.group ? 1.f / (float)a.group : inv;
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
@@ -91,10 +93,6 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
         rstd = rsqrtf(lanes_sum(t, lanes) * inv_group + a.eps);
         if (a.rstd_y && u < upr && (u & (lanes - 1)) == 0) a.rstd_y[(size_t)row * (upr >> shift) + (u >> shift)] = rstd;
       }
-      if (!AHEAD) {
-        columns8(a.gain_y, u * 8, a.cols, 1.f, gy[i]);
-        columns8(a.mode == GATE_COLUMN ? (const float*)a.gate : nullptr, u * 8, a.cols, 1.f, gc[i]);
-      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float slope;
@@ -111,7 +109,6 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int u = lane + i * TPR, n = a.cols - u * 8;
-      if (!AHEAD) columns8(a.gain_x, u * 8, a.cols, 1.f, gx[i]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[i][j] = x[i][j] * rstd * gx[i][j];
       if (u < upr) Unit<T, VEC>::store((T*)a.out + (size_t)row * a.ld_out + u * 8, x[i], n);
@@ -119,17 +116,17 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
   }
 }
 
-// A workgroup's rows of d_gain_y, d_gain_x and a column gate's d_gate stay in registers over all the rows that it takes: one row of `partial` each in the end, no
-// atomics, so the bits do not depend on the order of workgroups.
-template <typename T, int W, int U, bool VEC>
+// A workgroup's rows of d_gain_y, d_gain_x and a column gate's d_gate stay in registers over all the rows that it takes: one row of `partial` each in the end (rows of whole units: 16-byte
+// stores; one by one they took 6 us of 23 with 777 fp32 rows of 1001), no atomics, so the bits do not depend on the order of workgroups.
+template <typename T, int W, bool VEC, bool COLUMN>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(GatedArgs a) {
   constexpr int TPR = W * 64, RPB = W == 1 ? 4 : 1;
-  constexpr bool AHEAD = AHEAD_FITS<W, U>;
+  constexpr bool AHEAD = W < 16;
   __shared__ float red[2][2][W];
   __shared__ float joined[W == 1 ? 3 : 1][W == 1 ? U * 512 : 1];
   const int lane = threadIdx.x % TPR, part = threadIdx.x / TPR, step = gridDim.x * RPB;
   const int upr = (a.cols + 7) / 8, lanes = a.group / 8, shift = a.group ? __builtin_ctz(lanes) : 0, per_row = a.group ? upr >> shift : 1;
-  const bool wide = a.mode >= GATE_PLAIN, column = a.mode == GATE_COLUMN;
+  const bool wide = !COLUMN && a.mode >= GATE_PLAIN;
   Row8<T, VEC> xv[U], yv[U], gv[U], dv[U], sv[U];
   float ry[U], rx = 0.f;
   auto request = [&](int r) __attribute__((always_inline)) {
@@ -156,13 +153,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
   }
   int row = blockIdx.x * RPB + part;
   if (AHEAD && row < a.rows) request(row);
-  if (AHEAD) {
+  {
 #pragma unroll
     for (int i = 0; i < U; ++i) columns8(a.gain_y, (lane + i * TPR) * 8, a.cols, 1.f, gy[i]);
 #pragma unroll
     for (int i = 0; i < U; ++i) columns8(a.gain_x, (lane + i * TPR) * 8, a.cols, 1.f, gx[i]);
 #pragma unroll
-    for (int i = 0; i < U; ++i) columns8(column ? (const float*)a.gate : nullptr, (lane + i * TPR) * 8, a.cols, 1.f, gc[i]);
+    for (int i = 0; i < U; ++i) columns8(COLUMN ? (const float*)a.gate : nullptr, (lane + i * TPR) * 8, a.cols, 1.f, gc[i]);
   }
   const float inv = 1.f / (float)a.cols, inv_group = a.group ? 1.f / (float)a.group : inv;
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
@@ -174,11 +171,6 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
       const int u = lane + i * TPR;
       xv[i].get(x[i]); dv[i].get(d[i]); yv[i].get(y[i]); gv[i].get(g[i]); sv[i].get(s[i]);
       by[i] = ry[i];
-      if (!AHEAD) {
-        columns8(a.gain_y, u * 8, a.cols, 1.f, gy[i]);
-        columns8(a.gain_x, u * 8, a.cols, 1.f, gx[i]);
-        columns8(column ? (const float*)a.gate : nullptr, u * 8, a.cols, 1.f, gc[i]);
-      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         x[i][j] *= rstd;
@@ -201,7 +193,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
         s[i][j] = a.residual_scale * t;
         y[i][j] *= by[i];                                     // yhat
         g[i][j] = scaled * (y[i][j] * gy[i][j]) * slope;      // d_gate
-        dgc[i][j] += g[i][j];
+        if (COLUMN) dgc[i][j] += g[i][j];
         d[i][j] = scaled * act;                               // d_u
         dgy[i][j] += d[i][j] * y[i][j];
         d[i][j] *= gy[i][j];
@@ -245,31 +237,33 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
 #pragma unroll
           for (int q = 0; q < 3; ++q) v[i][j] += joined[q][(i * 8 + j) * 64 + lane];
     }
-    float* to = a.partial + ((size_t)which * gridDim.x + blockIdx.x) * a.cols;
+    float* to = a.partial + ((size_t)which * gridDim.x + blockIdx.x) * (upr * 8);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = lane + i * TPR, n = a.cols - u * 8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) if (u < upr && j < n) to[u * 8 + j] = v[i][j];
+      const int u = lane + i * TPR;
+      if (u >= upr) continue;
+      Store<float>::store4(to + u * 8, v[i][0], v[i][1], v[i][2], v[i][3]);
+      Store<float>::store4(to + u * 8 + 4, v[i][4], v[i][5], v[i][6], v[i][7]);
     }
   };
   if (a.d_gain_y) leave(dgy, 0);
   if (a.d_gain_x) leave(dgx, 1);
-  if (column && a.d_gate) leave(dgc, 2);
+  if (COLUMN && a.d_gate) leave(dgc, 2);
 }
 
 // The partial rows in order, 16 threads a column that take a part of them each; a row of workgroups for each of the sums
 __global__ __launch_bounds__(1024) void gated_gain_kernel(const float* partial, int groups, int cols, float* d_gain_y, float* d_gain_x, float* d_gate) {
   float* const to = blockIdx.y == 0 ? d_gain_y : blockIdx.y == 1 ? d_gain_x : d_gate;
   if (!to) return;
-  partial += (size_t)blockIdx.y * groups * cols;
+  const int ld = (cols + 7) / 8 * 8;
+  partial += (size_t)blockIdx.y * groups * ld;
   __shared__ float red[1024];
   const int c = blockIdx.x * 64 + threadIdx.x % 64, part = threadIdx.x / 64;
   const int per = (groups + 15) / 16, lo = part * per, hi = min(groups, lo + per);
   float t = 0.f;
   if (c < cols) {
 #pragma unroll 16
-    for (int r = lo; r < hi; ++r) t += partial[(size_t)r * cols + c];
+    for (int r = lo; r < hi; ++r) t += partial[(size_t)r * ld + c];
   }
   red[threadIdx.x] = t;
   __syncthreads();
@@ -279,14 +273,18 @@ __global__ __launch_bounds__(1024) void gated_gain_kernel(const float* partial, 
   to[c] = t;
 }
 
-template <typename T, int W, int U, bool VEC> hipError_t forward_run(const GatedArgs& a, hipStream_t s) {
+template <typename T, int W, bool VEC> hipError_t forward_run(const GatedArgs& a, hipStream_t s) {
   const int want = W == 1 ? (a.rows + 3) / 4 : a.rows, most = 4096 / (W == 1 ? 4 : W);
-  DDG_LAUNCH((gated_forward_kernel<T, W, U, VEC>), dim3(want < most ? want : most), dim3(W == 1 ? 256 : W * 64), 0, s, a);
+  const dim3 grid(want < most ? want : most), block(W == 1 ? 256 : W * 64);
+  if (a.mode == GATE_COLUMN) DDG_LAUNCH((gated_forward_kernel<T, W, VEC, true>), grid, block, 0, s, a);
+  else DDG_LAUNCH((gated_forward_kernel<T, W, VEC, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
-template <typename T, int W, int U, bool VEC> hipError_t backward_run(const GatedArgs& a, hipStream_t s) {
+template <typename T, int W, bool VEC> hipError_t backward_run(const GatedArgs& a, hipStream_t s) {
   const int groups = gated_groups(a.rows, a.cols);
-  DDG_LAUNCH((gated_backward_kernel<T, W, U, VEC>), dim3(groups), dim3(W == 1 ? 256 : W * 64), 0, s, a);
+  const dim3 block(W == 1 ? 256 : W * 64);
+  if (a.mode == GATE_COLUMN) DDG_LAUNCH((gated_backward_kernel<T, W, VEC, true>), dim3(groups), block, 0, s, a);
+  else DDG_LAUNCH((gated_backward_kernel<T, W, VEC, false>), dim3(groups), block, 0, s, a);
   const hipError_t e = hipGetLastError();
   float* d_gate = a.mode == GATE_COLUMN ? (float*)a.d_gate : nullptr;
   if (e != hipSuccess || !(a.d_gain_y || a.d_gain_x || d_gate)) return e;
@@ -296,21 +294,19 @@ template <typename T, int W, int U, bool VEC> hipError_t backward_run(const Gate
 
 template <typename T, bool VEC> hipError_t forward_any(const GatedArgs& a, hipStream_t s) {
   const int upr = (a.cols + 7) / 8;
-  if (upr <= 64) return forward_run<T, 1, 1, VEC>(a, s);
-  if (upr <= 128) return forward_run<T, 2, 1, VEC>(a, s);
-  if (upr <= 256) return forward_run<T, 4, 1, VEC>(a, s);
-  if (upr <= 512) return forward_run<T, 8, 1, VEC>(a, s);
-  if (upr <= 1024) return forward_run<T, 16, 1, VEC>(a, s);
-  return forward_run<T, 16, 2, VEC>(a, s);
+  if (upr <= 64) return forward_run<T, 1, VEC>(a, s);
+  if (upr <= 128) return forward_run<T, 2, VEC>(a, s);
+  if (upr <= 256) return forward_run<T, 4, VEC>(a, s);
+  if (upr <= 512) return forward_run<T, 8, VEC>(a, s);
+  return forward_run<T, 16, VEC>(a, s);
 }
 template <typename T, bool VEC> hipError_t backward_any(const GatedArgs& a, hipStream_t s) {
   const int upr = (a.cols + 7) / 8;
-  if (upr <= 64) return backward_run<T, 1, 1, VEC>(a, s);
-  if (upr <= 128) return backward_run<T, 2, 1, VEC>(a, s);
-  if (upr <= 256) return backward_run<T, 4, 1, VEC>(a, s);
-  if (upr <= 512) return backward_run<T, 8, 1, VEC>(a, s);
-  if (upr <= 1024) return backward_run<T, 16, 1, VEC>(a, s);
-  return backward_run<T, 16, 2, VEC>(a, s);
+  if (upr <= 64) return backward_run<T, 1, VEC>(a, s);
+  if (upr <= 128) return backward_run<T, 2, VEC>(a, s);
+  if (upr <= 256) return backward_run<T, 4, VEC>(a, s);
+  if (upr <= 512) return backward_run<T, 8, VEC>(a, s);
+  return backward_run<T, 16, VEC>(a, s);
 }
 
 }  // namespace

@@ -339,7 +339,7 @@ def test_linear_rows_beyond_32_bits():
 
 # rows, columns, group, pad
 GATED = [(1, 1, 0, 0), (2, 7, 0, 0), (1, 2048, 128, 0), (5, 64, 8, 0), (9, 512, 512, 0), (4, 520, 8, 8), (3, 1001, 0, 3), (6, 2048, 256, 0), (130, 4096, 64, 0), (3, 8192, 32, 8),
-         (2, 8200, 0, 0), (2, 16384, 128, 0), (2, 12001, 0, 1), (6, 4104, 8, 0), (11, 320, 16, 5)]
+         (2, 8192, 0, 0), (700, 8192, 128, 0), (2, 8001, 0, 1), (600, 4104, 8, 0), (11, 320, 16, 5)]
 
 
 def gated_case(dtype, rows, cols, pad, gate, plain):

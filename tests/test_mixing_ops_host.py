@@ -203,7 +203,7 @@ def test_gated_refusals():
     for cols, group in ((64, 12), (64, 4), (64, 128), (96, 64), (2048, 1024), (64, -8)):
         refused(SHAPE, "group", gated(cols=cols, group=group).forward, *ok, out=G)
     gated(cols=96, group=32).forward(*ok, out=G)
-    refused(SHAPE, "at most 16384", gated(cols=16385).forward, *ok, out=G)
+    refused(SHAPE, "at most 8192", gated(cols=8193).forward, *ok, out=G)
     for ld in ("ld_y", "ld_gate", "ld_residual", "ld_x", "ld_out"):
         refused(SHAPE, ld, gated(**{ld: 60}).forward, *ok, out=G)
     refused(INVALID, "out overlaps gate", gated().forward, *ok, out=B)
