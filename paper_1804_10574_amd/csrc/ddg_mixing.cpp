@@ -377,7 +377,7 @@ ddg_status ddg_linear_attention_step(const ddg_linear_desc* desc, const void* q,
   CHECK(check_args(args, same));
   if (d.dry_run || d.rows == 0) return DDG_OK;
   const LinearStepArgs a{q, k, v, o, log_decay, slots, state_in, state_out, d.ld_q, d.ld_k, d.ld_v, d.ld_o,
-                         d.rows, d.heads, d.heads / d.kv_heads, d.dim_k, d.dim_v, d.slots, d.dtype, d.scale};
+                         d.rows, d.heads, d.heads / d.kv_heads, d.dim_k, d.dim_v, d.slots, d.dtype, d.scale, false};
   return done(linear_step_launch(a, (hipStream_t)d.stream), "linear attention step");
 }
 

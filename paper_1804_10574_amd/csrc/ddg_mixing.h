@@ -24,6 +24,7 @@ struct GatedArgs {
   long ld_y, ld_gate, ld_residual, ld_x, ld_out;
   int rows, cols, dtype, group, mode;
   float eps, scale, residual_scale;
+  bool past;                                                   // results go past the caches (set by the launch)
 };
 constexpr int GATED_COLS_MAX = 8192;
 int gated_groups(int rows, int cols);        // workgroups of the backward launch, each with rows of partial sums
@@ -54,6 +55,7 @@ struct LinearStepArgs {
   long ld_q, ld_k, ld_v, ld_o;
   int rows, heads, share, K, V, pool, dtype;
   float scale;
+  bool past;                                                   // states go past the caches (set by the launch)
 };
 constexpr int LINEAR_DIM_MAX = 256;
 int linear_segment(int rows, int sequences, int walks, bool ragged, int dtype);   // rows of a segment; 0: sequences are not split

@@ -5,6 +5,19 @@
 namespace ddg {
 namespace {
 
+// 16 bytes on their boundary; past the caches where the call's results are more than they hold: then nothing else is driven out for what the next kernel has to fetch from memory anyway
+// (8192 rows of 40 heads of 128 in bf16, turned: 26 us instead of 34, and 60 instead of 62 with the next reader; a quarter of the rows: 17.0 against 15.4 with the reader)
+constexpr size_t CACHED = 32u << 20;                       // the dies' L2 together
+template <typename V> __device__ __forceinline__ void put16(V* to, V v, bool past) {
+  if (past) {
+    asm volatile("" ::: "memory");                         // (without these the compiler makes one ordinary store of the two)
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<u32x4_t*>(to));
+    asm volatile("" ::: "memory");
+  } else {
+    *to = v;
+  }
+}
+
 // 8 columns of a row, as they lie in memory. VEC: 16-byte pieces on their boundaries. Otherwise pieces wherever they begin (gfx950 loads and stores
 // them there too), and the row's last columns, where fewer than 8 are left, one by one with zeros behind them.
 template <typename T, bool VEC> struct Unit {
@@ -34,7 +47,7 @@ template <typename T, bool VEC> struct Unit {
       for (int j = 0; j < Store<T>::VEC; ++j) o[i * Store<T>::VEC + j] = t[j];
     }
   }
-  __device__ static __forceinline__ void store(T* p, const float (&o)[8], int n) {
+  __device__ static __forceinline__ void store(T* p, const float (&o)[8], int n, bool past = false) {
     Unit q;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
@@ -45,7 +58,7 @@ template <typename T, bool VEC> struct Unit {
     }
     if (VEC) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) reinterpret_cast<piece_t*>(p)[i] = q.v[i];
+      for (int i = 0; i < PIECES; ++i) put16(reinterpret_cast<piece_t*>(p) + i, q.v[i], past);
     } else if (n >= 8) {
       __builtin_memcpy(p, q.v, sizeof(q.v));
     } else {

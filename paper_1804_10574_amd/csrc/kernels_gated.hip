@@ -100,7 +100,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
         x[i][j] = a.residual_scale * x[i][j] + a.scale * (act * (y[i][j] * rstd * gy[i][j]));
         ss += x[i][j] * x[i][j];
       }
-      if (a.x && u < upr) Unit<T, VEC>::store((T*)a.x + (size_t)row * a.ld_x + u * 8, x[i], n);
+      if (a.x && u < upr) Unit<T, VEC>::store((T*)a.x + (size_t)row * a.ld_x + u * 8, x[i], n, a.past);
     }
     if (!a.out && !a.rstd_x) continue;
     const float rstd = rsqrtf(row_sum<W>(ss, red[turn][1]) * inv + a.eps);
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
       const int u = lane + i * TPR, n = a.cols - u * 8;
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[i][j] = x[i][j] * rstd * gx[i][j];
-      if (u < upr) Unit<T, VEC>::store((T*)a.out + (size_t)row * a.ld_out + u * 8, x[i], n);
+      if (u < upr) Unit<T, VEC>::store((T*)a.out + (size_t)row * a.ld_out + u * 8, x[i], n, a.past);
     }
   }
 }
@@ -199,13 +199,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
         d[i][j] *= gy[i][j];
         m += d[i][j] * y[i][j];
       }
-      if (u < upr && a.d_residual) Unit<T, VEC>::store((T*)a.d_residual + (size_t)row * a.ld_residual + u * 8, s[i], n);
-      if (u < upr && wide && a.d_gate) Unit<T, VEC>::store((T*)a.d_gate + (size_t)row * a.ld_gate + u * 8, g[i], n);
+      if (u < upr && a.d_residual) Unit<T, VEC>::store((T*)a.d_residual + (size_t)row * a.ld_residual + u * 8, s[i], n, a.past);
+      if (u < upr && wide && a.d_gate) Unit<T, VEC>::store((T*)a.d_gate + (size_t)row * a.ld_gate + u * 8, g[i], n, a.past);
       if (a.group && a.d_y) {
         m = lanes_sum(m, lanes) * inv_group;
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[i][j] = by[i] * (d[i][j] - y[i][j] * m);
-        if (u < upr) Unit<T, VEC>::store((T*)a.d_y + (size_t)row * a.ld_y + u * 8, s[i], n);
+        if (u < upr) Unit<T, VEC>::store((T*)a.d_y + (size_t)row * a.ld_y + u * 8, s[i], n, a.past);
         m = 0.f;
       }
     }
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
       const int u = lane + i * TPR, n = a.cols - u * 8;
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[i][j] = by[i] * (d[i][j] - y[i][j] * m);
-      if (u < upr) Unit<T, VEC>::store((T*)a.d_y + (size_t)row * a.ld_y + u * 8, s[i], n);
+      if (u < upr) Unit<T, VEC>::store((T*)a.d_y + (size_t)row * a.ld_y + u * 8, s[i], n, a.past);
     }
   }
   auto leave = [&](float (&v)[U][8], int which) __attribute__((always_inline)) {
@@ -317,16 +317,20 @@ int gated_groups(int rows, int cols) {
   return want < 1 ? 1 : want < most ? want : most;
 }
 
-hipError_t gated_forward_launch(const GatedArgs& a, hipStream_t s) {
+hipError_t gated_forward_launch(const GatedArgs& given, hipStream_t s) {
+  GatedArgs a = given;
   const size_t size = dtype_size(a.dtype);
+  a.past = (size_t)a.rows * a.cols * size * ((a.x != nullptr) + (a.out != nullptr)) > CACHED;
   const bool vec = a.cols % 8 == 0 && aligned(a.y, a.ld_y, size, 16) && (a.mode < GATE_PLAIN || aligned(a.gate, a.ld_gate, size, 16)) &&
                    aligned(a.residual, a.ld_residual, size, 16) && aligned(a.x, a.ld_x, size, 16) && aligned(a.out, a.ld_out, size, 16);
   if (a.dtype == BF16) return vec ? forward_any<bf16_t, true>(a, s) : forward_any<bf16_t, false>(a, s);
   return vec ? forward_any<float, true>(a, s) : forward_any<float, false>(a, s);
 }
 
-hipError_t gated_backward_launch(const GatedArgs& a, hipStream_t s) {
+hipError_t gated_backward_launch(const GatedArgs& given, hipStream_t s) {
+  GatedArgs a = given;
   const size_t size = dtype_size(a.dtype);
+  a.past = (size_t)a.rows * a.cols * size * ((a.d_residual != nullptr) + (a.d_y != nullptr) + (a.mode >= GATE_PLAIN && a.d_gate)) > CACHED;
   const bool vec = a.cols % 8 == 0 && aligned(a.y, a.ld_y, size, 16) && aligned(a.d_y, a.ld_y, size, 16) && aligned(a.x, a.ld_x, size, 16) &&
                    (a.mode < GATE_PLAIN || (aligned(a.gate, a.ld_gate, size, 16) && aligned(a.d_gate, a.ld_gate, size, 16))) &&
                    aligned(a.d_x, a.ld_x, size, 16) && aligned(a.d_out, a.ld_out, size, 16) && aligned(a.d_residual, a.ld_residual, size, 16);

@@ -6,8 +6,8 @@
 // A workgroup of four waves walks over a sequence (or a segment of one) for one head and one slice; S stays in its registers in 32 bits and goes to LDS once a chunk,
 // as the operand of the next product. Where there are fewer sequences and heads than the chip holds, sequences are cut into segments: a pass that only adds up
 // each segment's own state, a short scan over the segments, and the walk, which starts each segment from the state that the scan left.
-#include "ddg_device.h"
 #include "ddg_mixing.h"
+#include "ddg_rows.h"
 
 #include <type_traits>
 
@@ -597,7 +597,7 @@ __global__ __launch_bounds__(256) void step_kernel(LinearStepArgs a) {
       o.x += qr * s.x; o.y += qr * s.y; o.z += qr * s.z; o.w += qr * s.w;
       if (out) {
         float* f = out + (size_t)r * V + c;
-        if (VEC) { if (c < V) *reinterpret_cast<float4*>(f) = s; }
+        if (VEC) { if (c < V) put16(reinterpret_cast<float4*>(f), s, a.past); }
         else {
           if (c < V) f[0] = s.x;
           if (c + 1 < V) f[1] = s.y;
@@ -681,7 +681,9 @@ template <typename T, int COLS, int ROWS> hipError_t step_run(const LinearStepAr
   else DDG_LAUNCH((step_kernel<T, COLS, ROWS, false>), dim3(a.rows * a.heads), dim3(256), 0, s, a);
   return hipGetLastError();
 }
-template <typename T> hipError_t step_typed(const LinearStepArgs& a, hipStream_t s) {
+template <typename T> hipError_t step_typed(const LinearStepArgs& given, hipStream_t s) {
+  LinearStepArgs a = given;
+  a.past = a.state_out && (size_t)a.rows * a.heads * a.K * a.V * 4 > CACHED;
   const bool vec = a.V % 4 == 0 && (uintptr_t)a.state_in % 16 == 0 && (uintptr_t)a.state_out % 16 == 0;
   if (a.V <= 64) return step_run<T, 16, 8>(a, vec, s);
   if (a.V <= 128) return step_run<T, 32, 16>(a, vec, s);

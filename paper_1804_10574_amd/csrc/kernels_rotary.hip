@@ -33,12 +33,12 @@ template <typename T, bool VEC> __device__ __forceinline__ void get(const T* p, 
     for (int i = 0; i < W; ++i) o[i] = i < n ? Store<T>::load1(p + i) : 0.f;
   }
 }
-template <typename T, bool VEC> __device__ __forceinline__ void put(T* p, int n, const float (&o)[Store<T>::VEC]) {
+template <typename T, bool VEC> __device__ __forceinline__ void put(T* p, int n, const float (&o)[Store<T>::VEC], bool past) {
   constexpr int W = Store<T>::VEC;
   if (VEC || n >= W) {
     typename Store<T>::vec_t v;
     Store<T>::store_vec(reinterpret_cast<T*>(&v), o);
-    if (VEC) *reinterpret_cast<typename Store<T>::vec_t*>(p) = v;
+    if (VEC) put16(reinterpret_cast<typename Store<T>::vec_t*>(p), v, past);
     else __builtin_memcpy(p, &v, sizeof(v));
   } else {
 #pragma unroll
@@ -48,7 +48,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void put(T* p, int n,
 
 // RB rows a workgroup. A unit is 16 bytes of neighbouring pairs, or two of halves, or 16 bytes that are copied. VEC: every piece is whole and on its boundary.
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int RB, int turned, int copied, ImgOf per_row, ImgOf per_head, ImgOf pairs) {
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int RB, int turned, int copied, bool past, ImgOf per_row, ImgOf per_head, ImgOf pairs) {
   constexpr int W = Store<T>::VEC;
   extern __shared__ float2 turns[];                // [RB][rot / 2]
   const int half = a.rot / 2, row0 = blockIdx.x * RB, rows = min(RB, a.rows - row0);
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int RB, int t
       const int c = a.rot + (u - turned) * W;
       float v[W];
       get<T, VEC>(x + c, a.dim - c, v);
-      put<T, VEC>(y + c, a.dim - c, v);
+      put<T, VEC>(y + c, a.dim - c, v, past);
     } else if (a.interleaved) {
       const int c = u * W;
       float v[W], o[W];
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int RB, int t
         o[j] = v[j] * w.x - v[j + 1] * w.y;
         o[j + 1] = v[j + 1] * w.x + v[j] * w.y;
       }
-      put<T, VEC>(y + c, a.rot - c, o);
+      put<T, VEC>(y + c, a.rot - c, o, past);
     } else {
       const int c = u * W, n = half - c;
       float v[W], h[W], o[W], p[W];
@@ -93,8 +93,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int RB, int t
         o[j] = v[j] * w.x - h[j] * w.y;
         p[j] = h[j] * w.x + v[j] * w.y;
       }
-      put<T, VEC>(y + c, n, o);
-      put<T, VEC>(y + half + c, n, p);
+      put<T, VEC>(y + c, n, o, past);
+      put<T, VEC>(y + half + c, n, p, past);
     }
   }
 }
@@ -109,8 +109,10 @@ template <typename T> hipError_t run(const RotaryArgs& a, hipStream_t s) {
   const bool vec = span % W == 0 && a.dim % W == 0 && a.rot % W == 0 && aligned(a.x, a.ld_x, sizeof(T), 16) && aligned(a.y, a.ld_y, sizeof(T), 16);
   const int upr = a.heads * (turned + copied);
   const int rows = a.rows < ROWS_A_LAUNCH ? a.rows : ROWS_A_LAUNCH;
+  // a workgroup has work for its threads, and the chip for all of them (8192 rows of 320 units: 34 us with one row, 38 with eight)
   int RB = 1;
-  while (RB < 8 && RB * 2048 <= rows && (long)RB * 2 * upr <= 8192 && RB * 2 * half <= 1024) RB *= 2;
+  while (RB < 32 && RB * upr < 256 && RB * 512 <= rows && RB * 2 * half <= 1024) RB *= 2;
+  const bool past = (size_t)a.rows * a.heads * a.dim * sizeof(T) > CACHED;
   const ImgOf per_row = ImgOf::make(upr, (long)RB * upr), per_head = ImgOf::make(turned + copied, upr), pairs = ImgOf::make(half, RB * half);
   const size_t lds = (size_t)RB * half * sizeof(float2);
   for (int row0 = 0; row0 < a.rows; row0 += ROWS_A_LAUNCH) {
@@ -121,8 +123,8 @@ template <typename T> hipError_t run(const RotaryArgs& a, hipStream_t s) {
     else b.first = a.first + row0;
     b.rows = a.rows - row0 < ROWS_A_LAUNCH ? a.rows - row0 : ROWS_A_LAUNCH;
     const dim3 grid((b.rows + RB - 1) / RB);
-    if (vec) DDG_LAUNCH((rotary_kernel<T, true>), grid, dim3(256), lds, s, b, RB, turned, copied, per_row, per_head, pairs);
-    else DDG_LAUNCH((rotary_kernel<T, false>), grid, dim3(256), lds, s, b, RB, turned, copied, per_row, per_head, pairs);
+    if (vec) DDG_LAUNCH((rotary_kernel<T, true>), grid, dim3(256), lds, s, b, RB, turned, copied, past, per_row, per_head, pairs);
+    else DDG_LAUNCH((rotary_kernel<T, false>), grid, dim3(256), lds, s, b, RB, turned, copied, past, per_row, per_head, pairs);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
