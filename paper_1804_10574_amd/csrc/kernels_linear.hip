@@ -66,6 +66,13 @@ template <typename T, int DK> struct State {
   __device__ static __forceinline__ int at(int r, int p) { return r * DK + (p ^ (r / ROWS & (PLACES - 1))) * W; }
 };
 
+// Whether any of a piece's elements is infinite or NaN: all bits of its exponent are set
+__device__ __forceinline__ bool beyond(uint4 v) {
+  const auto carry = [](unsigned u) { return (u & 0x7f807f80u) + 0x00800080u; };     // (bf16 pairs: a set exponent's carry ends in the sign's place)
+  return ((carry(v.x) | carry(v.y) | carry(v.z) | carry(v.w)) & 0x80008000u) != 0;
+}
+__device__ __forceinline__ bool beyond(float4 v) { return !(fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY && fabsf(v.w) < INFINITY); }
+
 // b times the rows' weights, as N fragments whose sum it is: bf16 keeps 8 bits of the product in each, fp32 all of them
 template <int N> __device__ __forceinline__ void weigh(uint4 b, const float* w, uint4 (&o)[N]) {
   float v[8];
@@ -236,7 +243,7 @@ __global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 
   T* const bt = at + CHUNK * LDA;                          // [64][LDB]
   T* const st = bt + CHUNK * LDB;                          // [PLANES][State]
   __shared__ float pair_power[2 * CHUNK], row_power[2 * CHUNK];
-  __shared__ int counted[12];
+  __shared__ int counted[12], beyond_at[2];
 
   const LinearJob job = g.job[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
@@ -333,8 +340,9 @@ __global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 
   };
   weigh_rows(CHUNK);
 
+  if (tid < 2) beyond_at[tid] = 0;
   for (int r0 = 0; r0 < place.rows; r0 += CHUNK) {
-    const int n = min(CHUNK, place.rows - r0);
+    const int n = min(CHUNK, place.rows - r0), turn = r0 / CHUNK & 1;
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < PA; ++i) {
@@ -344,7 +352,14 @@ __global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       const int p = tid + i * 256, r = p / (SLICE / W), c = p % (SLICE / W) * W;
-      *reinterpret_cast<frag_t*>(bt + r * LDB + c) = rb.settle(br[i], r, c);
+      br[i] = rb.settle(br[i], r, c);
+      *reinterpret_cast<frag_t*>(bt + r * LDB + c) = br[i];
+    }
+    if (!SUM) {
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < PB; ++i) any |= beyond(br[i]);
+      if (any) beyond_at[turn] = 1;
     }
     if (!SUM) {
 #pragma unroll
@@ -366,6 +381,8 @@ __global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 
       for (int s = 0; s < STEPS; ++s) x[s] = rx.settle(x[s], row, s * M::KSTEP + l4 * W);
     }
     if (r0 + CHUNK < place.rows) request(r0 + CHUNK);
+    const int special = SUM ? 0 : beyond_at[turn];
+    if (!SUM && tid == 0) beyond_at[turn ^ 1] = 0;
     // the state after these rows (before their results, which do not wait for it)
     if (n < CHUNK) weigh_rows(n);
     const float keep = n == CHUNK ? keep_whole : power(n);
@@ -427,7 +444,26 @@ __global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 
             for (int t = 0; t < 4; ++t) o[t] = M::mma(b[t], of[p], o[t]);
         }
       };
-      if (tile == 0) mix(std::integral_constant<int, 1>());
+      if (__builtin_amdgcn_readfirstlane(special)) {       // a row of b holds an infinity or NaN, whose product with 0 is not 0: rows one at a time, each to those from itself on
+#pragma unroll 1
+        for (int j = 0; j < CHUNK; ++j) {
+          float p = 0.f;
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s) {
+            T e[W];
+            __builtin_memcpy(e, &x[s], sizeof(e));
+#pragma unroll
+            for (int i = 0; i < W; ++i) p += Store<T>::load1(e + i) * Store<T>::load1(at + j * LDA + s * M::KSTEP + l4 * W + i);
+          }
+          p += __shfl_xor(p, 16);
+          p += __shfl_xor(p, 32);
+          p *= pair_power[CHUNK - 1 - row + j];
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[t][e] += j <= row ? p * Store<T>::load1(bt + j * LDB + 16 * t + 4 * l4 + e) : 0.f;
+        }
+      } else if (tile == 0) mix(std::integral_constant<int, 1>());
       else if (tile == 1) mix(std::integral_constant<int, 2>());
       else if (tile == 2) mix(std::integral_constant<int, 3>());
       else mix(std::integral_constant<int, 4>());

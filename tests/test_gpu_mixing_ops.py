@@ -283,7 +283,7 @@ def test_linear_gradients_against_differences():
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_linear_nan_keeps_to_its_sequence_and_head(dtype):
-    """NaN in keys reaches later rows of its own sequence and heads only; in queries its own row; in values at most 31 rows before it as well."""
+    """NaN in keys reaches later rows of its own sequence and heads only; in queries its own row; an infinity in values its own column of these rows."""
     c = mixing(dtype, [100, 200, 50], 4, 2, 64, 64, states=True)
     torch = c.torch
     clean, o = c.space(350, 256), c.space(350, 256)
@@ -306,10 +306,36 @@ def test_linear_nan_keeps_to_its_sequence_and_head(dtype):
     c.v[170, 64 + 5] = float("inf")                            # row 70 of sequence 1, heads 2 and 3, one column
     run(o)
     same[:] = True
-    same[139:300, 2:] = False
+    same[164:300, 2:] = False                                  # (its chunk of 64 rows takes another order of sums)
     assert torch.equal(o.view(350, 4, 64)[same], clean.view(350, 4, 64)[same]) and not bool(o.view(350, 4, 64)[170, 2, 5].isfinite())
+    assert off(o.view(350, 4, 64)[164:170], clean.view(350, 4, 64)[164:170]) <= MIX[dtype]
     other = [j for j in range(64) if j != 5]
-    assert torch.equal(o.view(350, 4, 64)[:, :, other], clean.view(350, 4, 64)[:, :, other])
+    same[228:] = True
+    assert torch.equal(o.view(350, 4, 64)[same][:, other], clean.view(350, 4, 64)[same][:, other])
+    assert off(o.view(350, 4, 64)[:, :, other], clean.view(350, 4, 64)[:, :, other]) <= MIX[dtype]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("row", [0, 15, 16, 40, 63, 64, 100])
+def test_linear_gradients_of_rows_before_and_after_a_nan(dtype, row):
+    """NaN in d_o of a row reaches dq of that row alone, dk and dv of it and of rows before it; NaN in v dq of it and of later rows, and dk of its row alone."""
+    c = mixing(dtype, [130], 1, 1, 64, 64)
+    torch = c.torch
+
+    def run():
+        dq, dk, dv = c.space(130, 64), c.space(130, 64), c.space(130, 64)
+        c.op.backward(c.q, c.k, c.v, c.lam - 0.01, c.d_o, dq, dk, dv, workspace=c.ws(True))
+        return dq, dk, dv
+
+    bad = lambda t: [i for i in range(130) if not bool(t[i].isfinite().all())]  # noqa: E731
+    keep = c.d_o[row].clone()
+    c.d_o[row] = float("nan")
+    dq, dk, dv = run()
+    assert bad(dq) == [row] and bad(dk) == list(range(row + 1)) and bad(dv) == list(range(row + 1))
+    c.d_o[row] = keep
+    c.v[row] = float("inf")
+    dq, dk, dv = run()
+    assert bad(dq) == list(range(row, 130)) and bad(dk) == [row] and bad(dv) == []
 
 
 def test_linear_rows_beyond_32_bits():
