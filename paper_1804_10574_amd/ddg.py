@@ -576,6 +576,8 @@ class Rotary:
         return out
 
     def __call__(self, x, y, table, positions=None, first=0, inverse=False):
+        if isinstance(table, np.ndarray):
+            raise DDGError(1, "table must be on the device: copy what table() returns there once")
         _int32(positions, "positions")
         status = self._call(self._d, _ptr(x), _ptr(positions), first, _ptr(table), 1 if inverse else 0, _ptr(y))
         if status:

@@ -52,6 +52,7 @@ def test_rotary_refusals():
     refused(INVALID, "aligned", rot(), A, B, C_ + 4)
     refused(INVALID, "aligned", rot(), A + 1, B, C_)
     refused(INVALID, "int32", rot(), A, B, C_, positions=np.zeros(4, np.int64))
+    refused(INVALID, "on the device", rot(), A, B, rot().table())
     rot(ld_x=256, ld_y=256)(A, A + 256, C_)                    # queries beside keys
 
 
