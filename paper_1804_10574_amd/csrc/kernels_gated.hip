@@ -27,12 +27,15 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
   return v;
 }
 
-// The gate's factor and its slope
-__device__ __forceinline__ float gate_of(int mode, float g, float& slope) {
+// The gate's factor and its slope. With e = exp(-|g|) the sigmoid and what it lacks to 1 are 1 / (1 + e) and e / (1 + e), in one order or the other: neither is a difference, so
+// both are good where the gate is all but closed or open. Of bf16 rows by the instructions for exp2 and 1 / x (within 2^-23 (2 + |g|)), of fp32 ones to their last bits.
+template <typename T> __device__ __forceinline__ float gate_of(int mode, float g, float& slope) {
   if (mode <= GATE_PLAIN) { slope = 1.f; return g; }
-  const float sig = __builtin_amdgcn_rcpf(1.f + __expf(-g));     // (both within 2^-22 or so where the gate is open: below the roundings that follow)
-  if (mode == GATE_SIGMOID) { slope = sig * (1.f - sig); return sig; }
-  slope = sig * (1.f + g * (1.f - sig));
+  const float e = sizeof(T) == 2 ? __expf(-fabsf(g)) : expf(-fabsf(g));
+  const float large = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.f + e) : 1.f / (1.f + e), small = e * large;
+  const float sig = g < 0.f ? small : large, rest = g < 0.f ? large : small;
+  if (mode == GATE_SIGMOID) { slope = sig * rest; return sig; }
+  slope = sig * (1.f + g * rest);
   return g * sig;
 }
 
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_forward_kernel(Ga
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float slope;
-        const float act = wide ? gate_of(a.mode, g[i][j], slope) : gc[i][j];
+        const float act = wide ? gate_of<T>(a.mode, g[i][j], slope) : gc[i][j];
         x[i][j] = a.residual_scale * x[i][j] + a.scale * (act * (y[i][j] * rstd * gy[i][j]));
         ss += x[i][j] * x[i][j];
       }
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void gated_backward_kernel(G
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float slope = 1.f;
-        const float act = wide ? gate_of(a.mode, g[i][j], slope) : gc[i][j];
+        const float act = wide ? gate_of<T>(a.mode, g[i][j], slope) : gc[i][j];
         const float t = s[i][j] + rstd * (d[i][j] - x[i][j] * c), scaled = a.scale * t;
         s[i][j] = a.residual_scale * t;
         y[i][j] *= by[i];                                     // yhat

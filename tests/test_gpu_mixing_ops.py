@@ -436,6 +436,31 @@ def test_gated_backward(dtype, rows, cols, group, pad, gate, plain):
         assert torch.equal(d_x, d_res)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gate", ["sigmoid", "silu"])
+def test_gated_by_gates_that_are_all_but_open_or_closed(dtype, gate):
+    """Each element within its own roundings: a gate's distance from 0 or 1 is no difference of rounded numbers."""
+    torch, ddg, kind, t, gen, mk, space = setup(dtype)
+    rows, cols = 7, 96
+    y, d_x = mk(rows, cols), mk(rows, cols)
+    g = torch.linspace(-24, 24, rows * cols, device="cuda").reshape(rows, cols).to(y.dtype)
+    ry = torch.ones((rows, 1), device="cuda")
+    op = ddg.GatedJoin(rows, cols, kind, gate=gate)
+    d_gate, x = space(rows, cols), space(rows, cols)
+    op.backward(y, ry, g, None, None, None, None, d_x=d_x, d_gate=d_gate)
+    v, u, a = g.double(), y.double(), d_x.double()
+    sig, rest = 1 / (1 + torch.exp(-v)), 1 / (1 + torch.exp(v))
+    want = a * u * (sig * rest if gate == "sigmoid" else sig * (1 + v * rest))
+    size = (a * u).abs() * (sig * rest if gate == "sigmoid" else sig * (1 + v.abs() * rest))       # of the terms
+    # e is off by 2^-23 (2 + |g|) of itself with bf16 rows, |g| <= 24, by a step (2^-23) with fp32; nine more roundings of half a step or a step (1 / x): 36 and 10 steps
+    steps = 10 if dtype == "f32" else 36
+    assert bool(((d_gate.double() - want).abs() <= (0 if dtype == "f32" else 2.0 ** -8) * want.abs() + steps * 2.0 ** -23 * size).all())
+    # forward: x = act(g) y rstd; the sum of 96 squares in 14 roundings of half a step, of which the root keeps half, and the rest of rstd in six
+    op.forward(y, g, None, None, None, x_out=x)
+    want = (sig if gate == "sigmoid" else v * sig) * u * ((u * u).mean(1, keepdim=True) + 1e-6).rsqrt()
+    assert bool(((x.double() - want).abs() <= ((0 if dtype == "f32" else 2.0 ** -8) + (steps + 14) * 2.0 ** -23) * want.abs()).all())
+
+
 @pytest.mark.parametrize("rows", [0, 1])
 def test_gated_backward_of_few_rows_writes_the_sums(rows):
     torch, ddg, kind, t, gen, mk, space = setup("f32")
