@@ -232,7 +232,7 @@ __device__ __forceinline__ int on_die(int id, int total) {
 
 // SUM: only the state of the segment's own rows, for the scan. PLANES: fragments a weighted b is taken apart into.
 template <typename T, int DK, int PLANES, bool VEC, bool SUM>
-__global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 2 : 1) void walk_kernel(LinearArgs g) {
+__device__ __forceinline__ void walk(const LinearArgs& g) {
   typedef Mma<T> M;
   typedef Mix<T> X;
   typedef typename M::frag_t frag_t;
@@ -511,6 +511,15 @@ __global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 
     }
 }
 
+// TWO: jobs whose keys are much narrower than the launch's widest (the gradients' walks swap keys and values) walk in tiles of `narrower` columns (777 fp32 rows of 40 x 72: 25 us,
+// 29.5 in one width). A kernel of its own: the registers of a walk of 128 columns do not hold both (2 spilled, 3 % of it).
+constexpr int narrower(int DK) { return DK <= 64 ? 32 : DK <= 128 ? 64 : DK / 2; }
+template <typename T, int DK, int PLANES, bool VEC, bool SUM, bool TWO>
+__global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 2 : 1) void walk_kernel(LinearArgs g) {
+  if (TWO && g.job[blockIdx.y].K <= narrower(DK)) walk<T, TWO ? narrower(DK) : DK, PLANES, VEC, SUM>(g);
+  else walk<T, DK, PLANES, VEC, SUM>(g);
+}
+
 // The states before each segment from the segments' own, in place, and the last one: a thread four elements (or one, where a state is no whole number of fours), segments
 // in order
 template <int E>
@@ -654,23 +663,29 @@ __global__ __launch_bounds__(256) void step_kernel(LinearStepArgs a) {
   }
 }
 
-template <typename T, int DK, int PLANES, bool VEC, bool SUM> hipError_t walk_run(const LinearArgs& g, int jobs, hipStream_t s) {
+template <typename T, int DK, int PLANES, bool VEC, bool SUM, bool TWO> hipError_t walk_run(const LinearArgs& g, int jobs, hipStream_t s) {
   constexpr int LDA = DK + Mix<T>::PAD, LDB = SLICE + Mix<T>::PAD;
   constexpr size_t lds = (size_t)(CHUNK * LDA + CHUNK * LDB + (SUM ? 0 : Mix<T>::PLANES * SLICE * DK)) * sizeof(T);
-  static const hipError_t allowed = hipFuncSetAttribute((const void*)walk_kernel<T, DK, PLANES, VEC, SUM>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  static const hipError_t allowed = hipFuncSetAttribute((const void*)walk_kernel<T, DK, PLANES, VEC, SUM, TWO>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (allowed != hipSuccess) return allowed;
   int slices = 0;
   for (int j = 0; j < jobs; ++j) slices = g.job[j].slices > slices ? g.job[j].slices : slices;
-  DDG_LAUNCH((walk_kernel<T, DK, PLANES, VEC, SUM>), dim3((unsigned)(g.segments * g.heads * slices + 7) / 8 * 8, jobs), dim3(256), lds, s, g);
+  DDG_LAUNCH((walk_kernel<T, DK, PLANES, VEC, SUM, TWO>), dim3((unsigned)(g.segments * g.heads * slices + 7) / 8 * 8, jobs), dim3(256), lds, s, g);
   return hipGetLastError();
+}
+template <typename T, int DK, int PLANES, bool VEC, bool SUM> hipError_t walk_widths(const LinearArgs& g, int jobs, hipStream_t s) {
+  bool two = false;
+  for (int j = 0; j < jobs; ++j) two |= g.job[j].K <= narrower(DK);
+  if constexpr (DK > 32) if (two) return walk_run<T, DK, PLANES, VEC, SUM, true>(g, jobs, s);
+  return walk_run<T, DK, PLANES, VEC, SUM, false>(g, jobs, s);
 }
 template <typename T, int DK, bool VEC, bool SUM> hipError_t walk_planes(const LinearArgs& g, int jobs, hipStream_t s) {
   if constexpr (sizeof(T) == 4) {
-    return walk_run<T, DK, 1, VEC, SUM>(g, jobs, s);
+    return walk_widths<T, DK, 1, VEC, SUM>(g, jobs, s);
   } else {
     bool kept = false;
     for (int j = 0; j < jobs; ++j) kept |= g.job[j].state_out != nullptr;
-    return kept ? walk_run<T, DK, 3, VEC, SUM>(g, jobs, s) : walk_run<T, DK, 2, VEC, SUM>(g, jobs, s);
+    return kept ? walk_widths<T, DK, 3, VEC, SUM>(g, jobs, s) : walk_widths<T, DK, 2, VEC, SUM>(g, jobs, s);
   }
 }
 template <typename T, bool VEC, bool SUM> hipError_t walk_any(const LinearArgs& g, int jobs, hipStream_t s) {
@@ -730,8 +745,8 @@ template <typename T> hipError_t step_typed(const LinearStepArgs& given, hipStre
 }  // namespace
 
 // Two workgroups a compute unit are resident: fewer walks than that are cut, for as many (a prompt of 16384 rows, 16 heads of 128, bf16: 130 us in segments of 1024 rows, 140 of 512, 172
-// of 2048). A segment costs three passes over a state, so the shortest is three chunks (3010 ragged rows of 12 heads, 64 x 128: 35 us, 39 with two chunks, 44 with one; 58 uncut), of fp32,
-// whose chunks take longer, one (777 ragged rows, gradients: 67 us, 70 with two, 130 uncut). Nobody knows how long the longest of ragged sequences is: 2048 rows are the most.
+// of 2048). A segment costs three passes over a state, so the shortest is three chunks (3010 ragged rows of 12 heads, 64 x 128: 37 us, 42 with two chunks, 41 with one; 72 uncut), of fp32,
+// whose chunks take longer, one (777 ragged rows, gradients: 46 us, 60 with two, 90 uncut). Nobody knows how long the longest of ragged sequences is: 2048 rows are the most.
 int linear_segment(int rows, int sequences, int walks, bool ragged, int dtype) {
   const int length = ragged ? rows : rows / sequences, average = rows / sequences, least = dtype == BF16 ? 3 * CHUNK : CHUNK;
   const long have = (long)sequences * walks, most = have < 512 ? (512 + have - 1) / have : 1;     // segments of a sequence of average length
