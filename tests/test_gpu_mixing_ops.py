@@ -182,6 +182,13 @@ def test_linear_backward(dtype, lengths, heads, kv_heads, dim_k, dim_v, pad, sta
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim_k,dim_v,pad", [(64, 96, 0), (96, 24, 8), (128, 256, 0), (250, 60, 1), (16, 192, 0), (32, 48, 0), (30, 34, 5), (128, 64, 1)])
+@pytest.mark.parametrize("lengths", [[90], [800, 0, 70]])
+def test_linear_gradients_of_keys_and_values_of_unlike_width(dtype, lengths, dim_k, dim_v, pad):
+    test_linear_backward(dtype, lengths, 4, 2, dim_k, dim_v, pad, True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_linear_equal_sequences_need_no_starts(dtype):
     c = mixing(dtype, [150, 150, 150], 2, 2, 64, 64, states=True)
     torch = c.torch
