@@ -411,7 +411,8 @@ ddg_status ddg_vocab_loss(const ddg_vocab_desc* d, const void* h, const void* w,
  * those that turn `high` times or more over the trained context stay, those of `low` turns or fewer are divided.
  * The position of a row is first + positions[row] (int32), or first + row where positions is NULL; any sign. ddg_rotary_table writes the frequencies as 64-bit
  * fractions of a turn to HOST memory (rot / 2 of them); ddg_rotary takes them from device memory, where the caller copies them once. Angles are good
- * to 2^-32 of a turn at every position; cosines, sines and the turned pair are fp32, rounded once. inverse != 0 turns the other way: the gradient of the same call. y may be x (same ld); then
+ * to 2^-28 + |position| 2^-62 of a turn (2^-28: an eighth of a turn in fp32; 2^-62: four steps of the table, by parts with low <= high / 2); `first` lies within 2^48 of 0. Cosines,
+ * sines and the turned pair are fp32, rounded once. inverse != 0 turns the other way: the gradient of the same call. y may be x (same ld); then
  * columns from `rot` on are not touched. */
 typedef struct {
   int rows, heads, dim, dtype;   /* dim: at most 1024 */

@@ -144,6 +144,7 @@ ddg_status ddg_rotary(const ddg_rotary_desc* desc, const void* x, const int32_t*
   ddg_rotary_desc d;
   CHECK(rotary_desc(desc, &d));
   if (d.rows && (!x || !y || !table)) return fail(DDG_ERR_INVALID_ARG, "x, y and table must not be null");
+  if (first > ROTARY_FIRST_MAX || first < -ROTARY_FIRST_MAX) return fail(DDG_ERR_INVALID_ARG, "first = %ld must be within %ld of 0", first, ROTARY_FIRST_MAX);
   const size_t size = dtype_size(d.dtype);
   const Arg args[] = {{"y", y, d.rows, d.heads * d.dim, d.ld_y, size, true},
                       {"x", x, d.rows, d.heads * d.dim, d.ld_x, size, false},

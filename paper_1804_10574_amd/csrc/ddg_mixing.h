@@ -13,6 +13,7 @@ struct RotaryArgs {
   float magnitude;
 };
 constexpr int ROTARY_DIM_MAX = 1024;
+constexpr long ROTARY_FIRST_MAX = 1l << 48;    // four steps of the table make 2^-14 of a turn there, and sums with positions and rows stay inside 64 bits
 hipError_t rotary_launch(const RotaryArgs& a, hipStream_t s);
 
 enum Gate { GATE_NONE = 0, GATE_COLUMN = 1, GATE_PLAIN = 2, GATE_SIGMOID = 3, GATE_SILU = 4 };

@@ -1,7 +1,8 @@
 // Rotary positions: the pairs (a, b) of a head's first `rot` columns are turned by an angle that grows with the row's position,
 //   (a cos - b sin, b cos + a sin) * magnitude,   angle = position * theta_i,
 // backwards for the gradient. Pairs are neighbours (2i, 2i+1) or halves (i, i + rot/2).
-// The angle: a table holds theta_i / 2 pi as a 64-bit fraction of a turn, so position times that, modulo 2^64, is the exact fraction of the last turn: a position
+// The angle: a table holds theta_i / 2 pi as a 64-bit fraction of a turn, so position times that, modulo 2^64, is the exact fraction of the last turn for the table's theta_i (within four
+// steps of the true one: |position| 2^-62 of a turn), and fp32 takes what is left of a quarter to 2^-28: a position
 // of a million radians is as good as one of one (in fp32 that product alone is off by 0.03 radians, in 64-bit floating point it costs more than the rows do).
 // A workgroup forms the cosines and sines of its rows once, in LDS, for all heads. Bound by memory: 8192 rows of 40 heads of 128 in bf16 take 26 us (168 MB, 6.4 TB/s).
 #include "ddg_mixing.h"

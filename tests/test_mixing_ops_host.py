@@ -72,6 +72,33 @@ def test_rotary_table(kw):
         assert ratio[0] == 1.0 and abs(ratio[-1] * kw["factor"] - 1) < 1e-12 and any(1 / kw["factor"] + 1e-6 < r < 1 for r in ratio)
 
 
+@pytest.mark.parametrize("first", [(1 << 48) + 1, -(1 << 48) - 1, (1 << 62), -(1 << 63)])
+def test_rotary_refuses_positions_that_the_table_does_not_reach(first):
+    """A step of the table times the position has to stay a small part of a turn, and the sum with positions and rows inside 64 bits."""
+    refused(INVALID, "first", rot(), A, B, C_, first=first)
+    edge = (1 << 48) if first > 0 else -(1 << 48)
+    rot()(A, B, C_, first=edge)
+    rot()(A, B, C_, positions=D, first=edge)
+
+
+@pytest.mark.parametrize("dim,kw", [(128, dict()), (1024, dict(base=1.0001, factor=40.0, context=8192, low=0.0, high=0.5)), (80, dict(base=500000.0, factor=2.5)),
+                                    (90, dict(base=10.0, factor=1.7, context=4096, low=2.0, high=16.0)), (2, dict())])
+def test_rotary_table_is_within_four_steps(dim, kw):
+    """Frequencies in 64 digits, low <= high / 2. The table's are formed with 64 bits, 2^-64 relative for each rounding, of at most 0.16 of a turn, 0.16 steps: the power is good to 2^-63 and its
+    exponent's rounding is less than another (3), the turn's constant, the quotient and the product (3), the share that is kept: four operations on values up to twice its range (8), and its
+    complement, quotient and sum (3): 17 * 0.16 = 2.7, and half a step for the rounding to whole ones."""
+    from decimal import Decimal as N, localcontext
+    with localcontext() as c:
+        c.prec = 64
+        pi = N("3.14159265358979323846264338327950288419716939937510582097494459")
+        table = rot(dim=dim, **kw).table()
+        factor, context, low, high = (N(kw.get(k, v)) for k, v in (("factor", 1.0), ("context", 0), ("low", 1.0), ("high", 32.0)))
+        for i, got in enumerate(table):
+            theta = (N(kw.get("base", 10000.0)).ln() * -2 * i / dim).exp()
+            w = min(N(1), max(N(0), (context * theta / (2 * pi) - low) / (high - low))) if context else N(0)
+            assert abs(N(int(got)) - theta * (w + (1 - w) / factor) / (2 * pi) * 2 ** 64) <= 4
+
+
 # ---- linear attention ----------------------------------------------------------------------------
 
 def lin(rows=64, heads=4, dim_k=32, dim_v=48, dtype=BF16, **kw):
