@@ -3,6 +3,8 @@
 Bounds (2-norm of the difference over that of the result), from the formats: a bf16 result is rounded once, at most 2^-8 of each element. Linear attention of bf16
 operands keeps 16 bits of the products of two rows and of the state as operands: 2^-16 each of the terms, 2^-12 together where they are eight times the result. fp32, and states whatever the operands: sums of n terms in any
 order differ by about sqrt(n) 2^-24 of the norm of their terms, 1e-5 up to n = 2^14. Cosines and sines in fp32 are good to 2^-23, products and sum to 2^-24 each: 2^-21."""
+import math
+
 import pytest
 
 from tests import mixing_ref as R
@@ -63,6 +65,56 @@ def test_rotary_far_positions(dtype):
     near = space(len(positions), 128)
     op(x, near, table, first=far - 4)
     assert torch.equal(near.isfinite(), y.isfinite()) and not torch.equal(near, y)
+
+
+def turned_by_whole_numbers(torch, x, heads, dim, table, positions, inverse):
+    """Halves of x turned by position times the table's own fractions of a turn, modulo 2^64, formed exactly on the host."""
+    part = [[p * f % (1 << 64) / 2.0 ** 64 for f in table] for p in positions]
+    angle = (-2.0 if inverse else 2.0) * math.pi * torch.tensor(part, dtype=torch.float64, device=x.device)[:, None]
+    a, b = x.double().reshape(len(positions), heads, 2, dim // 2).unbind(2)
+    return torch.cat((a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()), -1).reshape(x.shape)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("first,given", [((1 << 40) + 7, False), (-(1 << 40) - 9, False), ((1 << 33) + 1, True), (-(1 << 35) + 3, True), ((1 << 48), False), (-(1 << 48), True),
+                                         ((1 << 31) - 2, False), (-(1 << 31) - 2, True)])
+def test_rotary_positions_past_32_bits(dtype, first, given):
+    """Every angle of first, and of first + positions, against whole numbers: what fp32 makes of an eighth of a turn (2^-28 of a turn, 2^-25 radians) is within TURN."""
+    torch, ddg, kind, t, gen, mk, space = setup(dtype)
+    print(f"case rotary {dtype} first {first} positions {given}", flush=True)
+    offsets = [0, 1, -1, (1 << 31) - 1, -(1 << 31), 65537, -12345678] if given else list(range(7))
+    rows, heads, dim = len(offsets), 2, 64
+    x = mk(rows, heads * dim)
+    op = ddg.Rotary(rows, heads, dim, kind)
+    host = op.table()
+    table = torch.from_numpy(host.view("int64")).cuda()
+    positions = torch.tensor(offsets, device="cuda", dtype=torch.int32) if given else None
+    for inverse in (False, True):
+        y = space(rows, heads * dim)
+        op(x, y, table, positions=positions, first=first, inverse=inverse)
+        want = turned_by_whole_numbers(torch, x, heads, dim, [int(f) for f in host], [first + p for p in offsets], inverse)
+        for r in range(rows):
+            assert off(y[r], want[r]) <= TURN[dtype], (r, offsets[r])
+
+
+def test_rotary_rows_of_two_launches():
+    """More rows than a launch takes (2^23): the second launch's positions go on where the first one's end, given or not."""
+    torch, ddg, kind, t, gen, mk, space = setup("bf16")
+    cut, dim = 1 << 23, 2
+    rows, first = cut + 1000, (1 << 40) - 5
+    x, y = mk(rows, dim), space(rows, dim)
+    op, tail = ddg.Rotary(rows, 1, dim, kind), ddg.Rotary(1000, 1, dim, kind)
+    host = op.table()
+    table = torch.from_numpy(host.view("int64")).cuda()
+    positions = torch.arange(rows, device="cuda", dtype=torch.int32) * 3 - 7
+    for p in (None, positions):
+        op(x, y, table, positions=p, first=first)
+        alone = space(1000, dim)
+        tail(x[cut:], alone, table, positions=None if p is None else p[cut:], first=first if p is not None else first + cut)
+        assert torch.equal(y[cut:], alone)
+        at = list(range(cut - 3, cut + 3)) + [0, 1, rows - 1]
+        want = turned_by_whole_numbers(torch, x[at], 1, dim, [int(host[0])], [first + (r if p is None else int(p[r])) for r in at], False)
+        assert off(y[at], want) <= TURN["bf16"]
 
 
 def test_rotary_keeps_scores_relative():
