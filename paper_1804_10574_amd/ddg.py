@@ -536,6 +536,25 @@ def _int32(t, name):
         raise DDGError(1, f"{name} must be int32, next to each other ({dtype}, strides {t.stride() if hasattr(t, 'stride') else t.strides})")
 
 
+def _on_device(t, name):
+    """Kernels fault on memory of the host that is not pinned."""
+    if isinstance(t, np.ndarray) or not (getattr(t, "is_cuda", True) or t.is_pinned()):
+        raise DDGError(1, f"{name} must be on the device: copy it there")
+
+
+def _index(t, name, count):
+    """`count` int32 numbers or more on the device, next to each other."""
+    try:
+        if t is None or t.is_cuda and t.numel() >= count and t.is_contiguous() and _is_int32(t.dtype):
+            return
+    except AttributeError:                                     # addresses, arrays
+        pass
+    _int32(t, name)
+    _on_device(t, name)
+    if hasattr(t, "numel") and t.numel() < count:
+        raise DDGError(1, f"{name} must be {count} or more numbers ({t.numel()})")
+
+
 class VocabLoss:
     """ddg_vocab_loss: softmax cross entropy over a vocabulary and its gradients, without the logits. unaligned: workspace_bytes
     leaves room for an h or w off 16 bytes."""
@@ -560,7 +579,7 @@ class VocabLoss:
 
 class Rotary:
     """ddg_rotary on [rows][heads * dim]; inverse=True on the error gradient is its backward pass. `table` is what table() returns, copied to
-    the device once; its 64-bit words may be of any 8-byte type there."""
+    the device once; its 64-bit words may be of any 8-byte type there, next to each other."""
 
     def __init__(self, rows, heads, dim, dtype, rot=0, interleaved=False, base=10000.0, factor=1.0, context=0, low=1.0, high=32.0, magnitude=1.0, ld_x=0,
                  ld_y=0, stream=None, dry_run=False):
@@ -568,6 +587,7 @@ class Rotary:
                                1 if dry_run else 0)
         lib = load_library()
         self._d, self._call, self._table = C.byref(self.desc), lib.ddg_rotary, lib.ddg_rotary_table
+        self._need = (rot or dim) // 2 * 8
 
     def table(self) -> np.ndarray:
         """The frequencies as 64-bit fractions of a turn, on the host."""
@@ -575,11 +595,21 @@ class Rotary:
         _check(self._table(self._d, _ptr(out)))
         return out
 
+    def _look_at(self, table):
+        _on_device(table, "table")
+        if hasattr(table, "element_size") and (table.element_size() != 8 or table.numel() * 8 < self._need or not table.is_contiguous()):
+            raise DDGError(1, f"table must be {self._need // 8} words of 64 bits, next to each other ({table.numel()} of {table.element_size()} bytes)")
+
     def __call__(self, x, y, table, positions=None, first=0, inverse=False):
-        if isinstance(table, np.ndarray):
-            raise DDGError(1, "table must be on the device: copy what table() returns there once")
-        _int32(positions, "positions")
-        status = self._call(self._d, _ptr(x), _ptr(positions), first, _ptr(table), 1 if inverse else 0, _ptr(y))
+        try:
+            source, words, target = x.data_ptr(), table.data_ptr(), y.data_ptr()
+            ready = table.is_cuda and table.itemsize == 8 and table.nbytes >= self._need and table.is_contiguous()
+        except AttributeError:                                 # addresses, arrays
+            source, words, target, ready = _ptr(x), _ptr(table), _ptr(y), False
+        if not ready:
+            self._look_at(table)
+        _index(positions, "positions", self.desc.rows)
+        status = self._call(self._d, source, _ptr(positions), first, words, 1 if inverse else 0, target)
         if status:
             _check(status)
 
@@ -600,8 +630,8 @@ class LinearAttention:
         return int(self._space(self._d, 1 if backward else 0))
 
     def forward(self, q, k, v, log_decay, o, starts=None, slots=None, state_in=None, state_out=None, workspace=None):
-        _int32(starts, "starts")
-        _int32(slots, "slots")
+        _index(starts, "starts", self.desc.sequences + 1)
+        _index(slots, "slots", self.desc.sequences)
         status = self._forward(self._d, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(starts), _ptr(slots), _ptr(state_in), _ptr(o), _ptr(state_out),
                                _ptr(workspace), _bytes(workspace))
         if status:
@@ -609,8 +639,8 @@ class LinearAttention:
 
     def backward(self, q, k, v, log_decay, d_o, dq=None, dk=None, dv=None, starts=None, slots=None, state_in=None, d_state_out=None, d_state_in=None,
                  workspace=None):
-        _int32(starts, "starts")
-        _int32(slots, "slots")
+        _index(starts, "starts", self.desc.sequences + 1)
+        _index(slots, "slots", self.desc.sequences)
         status = self._backward(self._d, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(starts), _ptr(slots), _ptr(state_in), _ptr(d_o), _ptr(d_state_out),
                                 _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_state_in), _ptr(workspace), _bytes(workspace))
         if status:
@@ -618,7 +648,7 @@ class LinearAttention:
 
     def step(self, q, k, v, log_decay, o, slots=None, state_in=None, state_out=None):
         """One row of every sequence."""
-        _int32(slots, "slots")
+        _index(slots, "slots", self.desc.rows)
         status = self._step(self._d, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(slots), _ptr(state_in), _ptr(o), _ptr(state_out))
         if status:
             _check(status)

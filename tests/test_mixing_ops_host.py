@@ -276,3 +276,63 @@ def test_sizes_that_no_index_holds_are_refused():
     refused(SHAPE, "at most", gated(rows=big, cols=8).forward, A, B, None, None, None, out=1 << 50)
     refused(SHAPE, "ld_gate", gated(ld_gate=big).forward, A, B, C_, D, E, out=G)
     refused(SHAPE, "too many heads", lin(heads=1 << 23).forward, A, B, C_, D, E)
+
+
+class OnDevice:
+    """What the binding asks of a tensor on the device: no GPU is needed to refuse one."""
+
+    is_cuda = True
+
+    def __init__(self, count, size, dtype="torch.int64", contiguous=True):
+        self.count, self.size, self.dtype, self.contiguous = count, size, dtype, contiguous
+
+    def data_ptr(self):
+        return C_
+
+    def numel(self):
+        return self.count
+
+    def element_size(self):
+        return self.size
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def stride(self):
+        return (1 if self.contiguous else 2,)
+
+
+def test_rotary_table_on_the_host_or_of_another_kind_is_refused():
+    import torch
+    op = rot()                                                 # heads of 64: 32 words
+    for host in (torch.from_numpy(op.table().view("int64")), op.table(), op.table().view("int64")):
+        refused(INVALID, "on the device", op, A, B, host)
+    op(A, B, OnDevice(32, 8))
+    op(A, B, OnDevice(40, 8, "torch.float64"))                 # (any 8-byte type, longer than needed)
+    for other in (OnDevice(32, 4, "torch.float32"), OnDevice(64, 4, "torch.int32"), OnDevice(32, 8, contiguous=False), OnDevice(31, 8)):
+        refused(INVALID, "table must be 32 words", op, A, B, other)
+    refused(INVALID, "table must be 10 words", rot(rot=20), A, B, OnDevice(9, 8))
+    rot(rot=20)(A, B, OnDevice(10, 8))
+
+
+def test_whole_numbers_on_the_host_or_too_few_are_refused():
+    import torch
+    few, int32 = OnDevice(3, 4, "torch.int32"), OnDevice(5, 4, "torch.int32")
+    for host in (torch.zeros(8, dtype=torch.int32), np.zeros(8, np.int32)):
+        refused(INVALID, "positions must be on the device", rot(), A, B, C_, positions=host)
+        refused(INVALID, "starts must be on the device", lin(sequences=2).forward, A, B, C_, D, E, starts=host)
+        refused(INVALID, "slots must be on the device", lin(sequences=2).forward, A, B, C_, D, E, slots=host)
+        refused(INVALID, "starts must be on the device", lin(sequences=2).backward, A, B, C_, D, E, dq=F, starts=host)
+        refused(INVALID, "slots must be on the device", lin(sequences=2).backward, A, B, C_, D, E, dq=F, slots=host)
+        refused(INVALID, "slots must be on the device", lin(rows=4).step, A, B, C_, D, E, slots=host)
+    rot(rows=5)(A, B, D, positions=int32)
+    refused(INVALID, "positions must be 4 or more", rot(), A, B, D, positions=few)
+    lin(sequences=4).forward(A, B, F, D, E, starts=int32)
+    refused(INVALID, "starts must be 4 or more", lin(sequences=3).forward, A, B, F, D, E, starts=few)
+    refused(INVALID, "starts must be 4 or more", lin(sequences=3).backward, A, B, F, D, E, dq=G, starts=few)
+    refused(INVALID, "slots must be 4 or more", lin(sequences=4).forward, A, B, F, D, E, slots=few)
+    refused(INVALID, "slots must be 4 or more", lin(sequences=4).backward, A, B, F, D, E, dq=G, slots=few)
+    lin(rows=5, sequences=1).step(A, B, F, D, E, slots=int32)
+    refused(INVALID, "slots must be 6 or more", lin(rows=6, sequences=1).step, A, B, F, D, E, slots=int32)
+    refused(INVALID, "int32", lin(sequences=2).forward, A, B, F, D, E, starts=OnDevice(5, 8))
+    refused(INVALID, "int32", rot(), A, B, D, positions=OnDevice(5, 4, "torch.int32", contiguous=False))
