@@ -449,8 +449,9 @@ typedef struct {
   void* stream;
   int dry_run;
 } ddg_linear_desc;
-/* Bytes of the workspace (256-byte aligned): states between the segments that few long sequences are cut into (0 where they are not), in the backward pass three times
- * that, and where heads share keys the fp32 gradients of every head. 0 too if the descriptor is refused. */
+/* Bytes of the workspace (256-byte aligned): states between the segments that sequences longer than one are cut into, for as many as the rows allow (with `starts` the host does not know
+ * them: up to a state for every 96 rows (bf16; fp32: 32), however many sequences; 0 where the rows are one segment), in the backward pass three times that, and where heads share keys the
+ * fp32 gradients of every head. 0 too if the descriptor is refused. */
 size_t ddg_linear_attention_workspace(const ddg_linear_desc* d, int backward);
 ddg_status ddg_linear_attention(const ddg_linear_desc* d, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* starts,
                                 const int32_t* slots, const float* state_in, void* o, float* state_out, void* workspace, size_t workspace_bytes);

@@ -81,14 +81,17 @@ ddg_status linear_desc(const ddg_linear_desc* in, ddg_linear_desc* d) {
 
 long slices_of(int cols) { return (cols + 63) / 64; }
 
-// The cut into segments of a call
-struct Cut { int segment; long segments; size_t pieces; };
+// The cut into segments of a call, and the bytes of the states between them. Sequence n of a ragged call begins with piece start / segment + n; where that may lead past twice the rows, with
+// piece 2 start / segment instead: a sequence of several segments has more than one segment's rows, so at least as many numbers as segments, and the others need none.
+struct Cut { int segment; long segments; size_t pieces; bool by_rows; };
 Cut cut_of(const ddg_linear_desc& d, bool backward, bool ragged) {
   const long k = slices_of(d.dim_k), v = slices_of(d.dim_v), walks = d.heads * (backward ? 2 * k + v : v);
   Cut c;
   c.segment = linear_segment(d.rows, d.sequences, (int)(walks < (1 << 30) ? walks : 1 << 30), ragged, d.dtype);
   c.segments = !c.segment ? d.sequences : ragged ? d.rows / c.segment + (long)d.sequences : (long)d.sequences * ((d.rows / d.sequences + c.segment - 1) / c.segment);
-  c.pieces = c.segment ? (size_t)c.segments * d.heads * d.dim_k * d.dim_v * 4 : 0;
+  const long most = c.segment && ragged ? 2l * d.rows / c.segment : c.segments;
+  c.by_rows = most < c.segments;
+  c.pieces = c.segment ? (size_t)(c.by_rows ? most : c.segments) * d.heads * d.dim_k * d.dim_v * 4 : 0;
   c.pieces = (c.pieces + 255) / 256 * 256;
   return c;
 }
@@ -109,7 +112,7 @@ LinearArgs linear_args(const ddg_linear_desc& d, const Cut& c, const float* log_
   LinearArgs a{};
   a.log_decay = log_decay; a.starts = starts; a.slots = slots;
   a.rows = d.rows; a.sequences = d.sequences; a.heads = d.heads; a.pool = d.slots; a.dtype = d.dtype;
-  a.segment = c.segment ? c.segment : 1; a.segments = (int)c.segments; a.split = c.segment != 0;
+  a.segment = c.segment ? c.segment : 1; a.segments = (int)c.segments; a.split = c.segment != 0; a.by_rows = c.by_rows;
   return a;
 }
 

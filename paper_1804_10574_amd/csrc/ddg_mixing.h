@@ -43,13 +43,13 @@ struct LinearJob {
   float inter, intra, update;
   const float* state_in; float* state_out;                     // element (k, v) at k * at_k + v * at_v of a head's K * V
   long at_k, at_v;
-  float* pieces;                                               // [segments][heads][K][V]: states before each segment
+  float* pieces;                                               // [pieces][heads][K][V]: states before each segment of a sequence that has several
 };
 struct LinearArgs {
   LinearJob job[3];
   const float* log_decay; const int* starts; const int* slots;
   int rows, sequences, heads, pool, segment, segments, dtype;  // segment: rows of one; segments: most there can be
-  bool split;                                                  // sequences may have several segments
+  bool split, by_rows;                                         // sequences may have several segments; their pieces are numbered by rows alone
 };
 struct LinearStepArgs {
   const void* q; const void* k; const void* v; void* o; const float* log_decay; const int* slots; const float* state_in; float* state_out;

@@ -165,11 +165,11 @@ template <typename T> struct Rows<T, false> {
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Where a workgroup is: its sequence, and the rows [first, first + rows) of it, counted in the direction of the walk
-struct Place { int sequence, start, length, first, rows, segments; bool none; };
+struct Place { int sequence, start, length, first, rows, segments, piece; bool none; };
 
 __device__ __forceinline__ int clamp_row(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
 // Segments are numbered so that nobody has to add up lengths: sequence n's are start / segment + n and on, at least one each, and the numbers between are nobody's.
-// starts is device data that the host has not seen: everything is held inside [0, rows].
+// starts is device data that the host has not seen: everything is held inside [0, rows]. Pieces (states before the segments) have numbers of their own where by_rows says so.
 __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shared) {
   Place p;
   if (!g.starts) {
@@ -179,6 +179,7 @@ __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shar
     p.length = length;
     p.first = (number - p.sequence * each) * g.segment;
     p.segments = each;
+    p.piece = number;
     p.none = p.sequence >= g.sequences;
   } else if (!g.split) {
     p.sequence = number;
@@ -186,6 +187,7 @@ __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shar
     p.length = max(0, clamp_row(g.starts[number + 1], g.rows) - p.start);
     p.first = 0;
     p.segments = 1;
+    p.piece = number;
     p.none = false;
   } else {
     int before = 0, start = 0, end = 0;
@@ -212,6 +214,7 @@ __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shar
     p.length = max(0, shared[3 * w + 2] - p.start);
     p.first = (int)min((long)(number - (p.start / g.segment + n)) * g.segment, (long)g.rows);
     p.segments = max(1, (p.length + g.segment - 1) / g.segment);
+    p.piece = g.by_rows ? 2 * p.start / g.segment + p.first / g.segment : number;
     p.none |= p.first < 0 || (p.first > 0 && p.first >= p.length);     // (starts that fall are found anywhere)
   }
   p.sequence = __builtin_amdgcn_readfirstlane(p.sequence);
@@ -219,6 +222,7 @@ __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shar
   p.length = __builtin_amdgcn_readfirstlane(p.length);
   p.first = __builtin_amdgcn_readfirstlane(p.first);
   p.segments = __builtin_amdgcn_readfirstlane(p.segments);
+  p.piece = __builtin_amdgcn_readfirstlane(p.piece);
   p.rows = p.length - p.first;
   if (g.split && p.rows > g.segment) p.rows = g.segment;
   return p;
@@ -251,8 +255,7 @@ __device__ __forceinline__ void walk(const LinearArgs& g) {
   const int total = g.segments * g.heads * job.slices;
   if ((int)blockIdx.x >= total) return;
   const int number = on_die(blockIdx.x, total), slice = number % job.slices, head = number / job.slices % g.heads;
-  const size_t segment = (size_t)(number / job.slices / g.heads);
-  const Place place = find(g, (int)segment, counted);
+  const Place place = find(g, number / job.slices / g.heads, counted);
   if (place.none || (SUM && place.segments == 1)) return;
   const int K = job.K, V = job.V, v0 = slice * SLICE;
 
@@ -307,7 +310,7 @@ __device__ __forceinline__ void walk(const LinearArgs& g) {
     const float* from = nullptr;
     long rk = job.at_k, rv = job.at_v;
     if (!SUM && place.segments > 1) {
-      from = job.pieces + (segment * g.heads + head) * K * V;
+      from = job.pieces + ((size_t)place.piece * g.heads + head) * K * V;
       rk = V; rv = 1;
     } else if (!SUM && job.state_in && slot >= 0) {
       from = job.state_in + ((size_t)slot * g.heads + head) * K * V;
@@ -496,7 +499,7 @@ __device__ __forceinline__ void walk(const LinearArgs& g) {
   float* to = nullptr;
   long rk = job.at_k, rv = job.at_v;
   if (SUM) {
-    to = job.pieces + (segment * g.heads + head) * K * V;
+    to = job.pieces + ((size_t)place.piece * g.heads + head) * K * V;
     rk = V; rv = 1;
   } else if (place.segments == 1 && job.state_out && slot >= 0) {
     to = job.state_out + ((size_t)slot * g.heads + head) * K * V;
@@ -531,7 +534,7 @@ __global__ __launch_bounds__(256) void scan_kernel(LinearArgs g, int blocks) {
   if (g.starts) {
     start = clamp_row(g.starts[n], g.rows);
     length = max(0, clamp_row(g.starts[n + 1], g.rows) - start);
-    first = start / g.segment + n;
+    first = g.by_rows ? 2 * start / g.segment : start / g.segment + n;
   } else {
     length = g.rows / g.sequences;
     first = n * max(1, (length + g.segment - 1) / g.segment);

@@ -240,6 +240,26 @@ def test_linear_gradients_of_keys_and_values_of_unlike_width(dtype, lengths, dim
     test_linear_backward(dtype, lengths, 4, 2, dim_k, dim_v, pad, True)
 
 
+# more sequences than segments, so that states between segments are numbered by rows; long ones next to each other, between short and empty ones, and a row more than whole segments
+MANY = [1] * 150 + [500, 0, 401] + [0] * 40 + [2] * 100 + [193, 64, 65, 129, 0, 385] + [1] * 200
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv_heads,dim_k,dim_v,pad", [(2, 1, 16, 24, 0), (3, 3, 64, 100, 8)])
+def test_linear_many_short_sequences_and_a_few_long(dtype, heads, kv_heads, dim_k, dim_v, pad):
+    test_linear_forward(dtype, MANY, heads, kv_heads, dim_k, dim_v, pad, True)
+    test_linear_backward(dtype, MANY, heads, kv_heads, dim_k, dim_v, pad, True)
+    c = mixing(dtype, MANY, heads, kv_heads, dim_k, dim_v, pad, states=True)
+    o, dq = c.space(c.rows, heads * dim_v, pad), c.space(c.rows, heads * dim_k, pad)
+    for backward in (False, True):
+        need, ws = c.op.workspace_bytes(backward), c.ws(backward)
+        if backward:
+            c.op.backward(c.q, c.k, c.v, c.lam, c.d_o, dq=dq, starts=c.starts, state_in=c.states, d_state_out=c.d_states, workspace=ws[:need])
+        else:
+            c.op.forward(c.q, c.k, c.v, c.lam, o, starts=c.starts, state_in=c.states, workspace=ws[:need])
+        assert need and bool((ws[need:] == 255).all())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_linear_equal_sequences_need_no_starts(dtype):
     c = mixing(dtype, [150, 150, 150], 2, 2, 64, 64, states=True)

@@ -168,6 +168,18 @@ def test_linear_workspace():
     assert max(need, both) < 3.1 * 4 * 32 * 48 * 4 * (1 << 16) / 192 + 4096   # pieces: at most one per 192 rows
 
 
+@pytest.mark.parametrize("dtype,shortest", [(BF16, 192), (F32, 64)])
+@pytest.mark.parametrize("rows,sequences", [(8192, 64), (65536, 512), (4096, 4096), (100000, 65536), (8192, 1), (1000, 5000)])
+def test_linear_workspace_does_not_grow_with_sequences(dtype, shortest, rows, sequences):
+    """Only sequences longer than a segment need states between segments: there are at most two for every segment of the rows, however many sequences."""
+    op = lin(rows=rows, heads=8, dim_k=64, dim_v=96, dtype=dtype, sequences=sequences)
+    state = 8 * 64 * 96 * 4
+    most = max(2 * rows // shortest, 2) * state + 255
+    assert op.workspace_bytes() <= most and op.workspace_bytes(True) <= 3 * most
+    need = op.workspace_bytes()
+    op.forward(A, B, C_, D, E, starts=G, workspace=Space(need, 1 << 45))
+
+
 def test_linear_backward_refusals():
     op = lin()
     ok = (A, B, C_, D, E)
