@@ -170,7 +170,7 @@ struct Place { int sequence, start, length, first, rows, segments, piece; bool n
 __device__ __forceinline__ int clamp_row(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
 // Segments are numbered so that nobody has to add up lengths: sequence n's are start / segment + n and on, at least one each, and the numbers between are nobody's.
 // starts is device data that the host has not seen: everything is held inside [0, rows]. Pieces (states before the segments) have numbers of their own where by_rows says so.
-__device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shared) {
+__device__ __forceinline__ Place find(const LinearArgs& g, int number) {
   Place p;
   if (!g.starts) {
     const int length = g.rows / g.sequences, per = g.split ? (length + g.segment - 1) / g.segment : 1, each = per > 0 ? per : 1;
@@ -190,28 +190,26 @@ __device__ __forceinline__ Place find(const LinearArgs& g, int number, int* shar
     p.piece = number;
     p.none = false;
   } else {
-    int before = 0, start = 0, end = 0;
-    for (int n0 = 0; n0 < g.sequences; n0 += 256) {
-      const int n = min(n0 + (int)threadIdx.x, g.sequences - 1), s0 = clamp_row(g.starts[n], g.rows), s1 = clamp_row(g.starts[n + 1], g.rows);
-      const bool is = n == n0 + (int)threadIdx.x && s0 / g.segment + n <= number;
-      const int here = __popcll(__ballot(is));
-      before += here;
-      if (here) {                                          // the last one that begins at or before this number, in this wave
-        start = __shfl(s0, here - 1);
+    // the last sequence whose first number is this one or less; every wave looks for itself, at 64 of them in a trip (they rise; where starts fall, the range still shrinks). 65536 sequences of
+    // two rows, 2 heads of 64: 2.1 ms, 25 where every workgroup reads all starts; 4096, 8 heads: 0.51 ms, 0.82
+    int n = 0, end = 0;
+    p.start = 0;
+    p.none = false;
+    for (int span = g.sequences, step; ; span = step) {
+      step = (span + 63) / 64;
+      const int lane = threadIdx.x & 63, of = (int)min((long)n + (long)lane * step, (long)g.sequences - 1);
+      const int s0 = clamp_row(g.starts[of], g.rows), s1 = step == 1 ? clamp_row(g.starts[of + 1], g.rows) : 0;
+      const int here = __popcll(__ballot(lane * step < span && n + lane * step < g.sequences && s0 / g.segment + of <= number));
+      if (here == 0) { p.none = true; break; }
+      n += (here - 1) * step;
+      if (step == 1) {
+        p.start = __shfl(s0, here - 1);
         end = __shfl(s1, here - 1);
+        break;
       }
     }
-    if ((threadIdx.x & 63) == 0) {
-      const int w = threadIdx.x >> 6;
-      shared[3 * w] = before; shared[3 * w + 1] = start; shared[3 * w + 2] = end;
-    }
-    __syncthreads();
-    before = shared[0] + shared[3] + shared[6] + shared[9];
-    p.sequence = before - 1;
-    p.none = before < 1;
-    const int n = max(0, p.sequence), w = n >> 6 & 3;
-    p.start = shared[3 * w + 1];
-    p.length = max(0, shared[3 * w + 2] - p.start);
+    p.sequence = n;
+    p.length = max(0, end - p.start);
     p.first = (int)min((long)(number - (p.start / g.segment + n)) * g.segment, (long)g.rows);
     p.segments = max(1, (p.length + g.segment - 1) / g.segment);
     p.piece = g.by_rows ? 2 * p.start / g.segment + p.first / g.segment : number;
@@ -248,14 +246,15 @@ __device__ __forceinline__ void walk(const LinearArgs& g) {
   T* const bt = at + CHUNK * LDA;                          // [64][LDB]
   T* const st = bt + CHUNK * LDB;                          // [PLANES][State]
   __shared__ float pair_power[2 * CHUNK], row_power[2 * CHUNK];
-  __shared__ int counted[12], beyond_at[2];
+  __shared__ int beyond_at[2];
 
   const LinearJob job = g.job[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
   const int total = g.segments * g.heads * job.slices;
   if ((int)blockIdx.x >= total) return;
   const int number = on_die(blockIdx.x, total), slice = number % job.slices, head = number / job.slices % g.heads;
-  const Place place = find(g, number / job.slices / g.heads, counted);
+  const Place place = find(g, number / job.slices / g.heads);
+  if constexpr (!VEC && !SUM && sizeof(T) == 2) asm volatile("" ::: "memory");     // (else the compiler moves loads into the search, and unaligned rows of 128 columns spill 25 registers instead of 6)
   if (place.none || (SUM && place.segments == 1)) return;
   const int K = job.K, V = job.V, v0 = slice * SLICE;
 

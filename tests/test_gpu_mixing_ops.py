@@ -261,6 +261,24 @@ def test_linear_many_short_sequences_and_a_few_long(dtype, heads, kv_heads, dim_
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("count", [63, 64, 65, 4097])
+def test_linear_finds_its_sequence_among_many(dtype, count):
+    """Sequences are searched 64 at a time: one, two and three trips; long ones first, last and at the borders of a trip, empty ones between."""
+    lengths = [(0, 1, 1, 2)[i % 4] for i in range(count)]
+    for n, length in ((0, 401), (1, 0), (62, 130), (63, 65), (64, 200), (65, 64), (2048, 129), (4095, 330), (4096, 140)):
+        if n < count:
+            lengths[n] = length
+    lengths[-1] = 270
+    c = mixing(dtype, lengths, 1, 1, 16, 24, behind=1, states=True)
+    o, after = c.space(c.rows, 24), c.torch.full_like(c.states, 7.0)
+    c.op.forward(c.q, c.k, c.v, c.lam - 0.02, o, starts=c.starts, state_in=c.states, state_out=after, workspace=c.ws())
+    c.lam = c.lam - 0.02
+    want, want_after = reference(c)
+    assert off(o[:-1], want) <= MIX[dtype] and bool((o[-1] == 7.0).all())
+    assert off(after[:count], want_after[:count]) <= SUMS
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_linear_equal_sequences_need_no_starts(dtype):
     c = mixing(dtype, [150, 150, 150], 2, 2, 64, 64, states=True)
     torch = c.torch
