@@ -439,7 +439,7 @@ ddg_status ddg_rotary(const ddg_rotary_desc* d, const void* x, const int32_t* po
  * state is not kept. The slots of a call must differ. state_in NULL: S0 = 0; state_out: NULL or state_in itself or another pool; slots that no
  * sequence names are not written. States and sums are fp32; with bf16 operands the weighted rows that make a kept state are taken apart into three bf16 pieces (two
  * where none is kept, so the last bits of o depend on whether state_out is given, and those of dq, dk and dv on whether d_state_in is), the state and the products q.k as operands into two: o is
- * rounded once (a state or product past 3.39e38, bf16's largest value, counts as infinite there). An infinity or NaN in a row reaches results of that row and of later ones alone; of the
+ * rounded once (a state or product past 3.39e38, bf16's largest value, gives NaN). An infinity or NaN in a row reaches results of that row and of later ones alone; of the
  * gradients dq likewise, and dk, dv and d_state_in from the other end: a row of q or d_o reaches those of itself and of earlier rows. In a kept state an infinity with bf16 operands may be NaN.
  * At most 2^23 rows; dim_k and dim_v at most 256. */
 typedef struct {

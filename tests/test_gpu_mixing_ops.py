@@ -234,6 +234,56 @@ def test_linear_backward(dtype, lengths, heads, kv_heads, dim_k, dim_v, pad, sta
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths", [[90], [800, 0, 70], [1, 2]])
+@pytest.mark.parametrize("heads,kv_heads,dim_k,dim_v,pad", [(4, 2, 64, 96, 0), (2, 2, 96, 24, 8), (4, 1, 33, 60, 3), (2, 2, 128, 128, 0), (3, 3, 40, 72, 1)])
+def test_linear_gradient_of_the_first_state_alone(dtype, lengths, heads, kv_heads, dim_k, dim_v, pad):
+    """The walk has no results but the state: of heads that share keys or not, whole and cut, aligned or not. And the same as beside the other gradients."""
+    c = mixing(dtype, lengths, heads, kv_heads, dim_k, dim_v, pad, behind=2, states=True, seed=5)
+    print(f"case d_state_in alone {dtype} {lengths} {heads}/{kv_heads} {dim_k} {dim_v} +{pad}", flush=True)
+    torch, n = c.torch, sum(lengths)
+    for x in (c.q, c.k, c.v, c.d_o):
+        x[n:] = float("nan")
+    kw = dict(starts=c.starts, state_in=c.states, d_state_out=c.d_states, workspace=c.ws(True))
+    alone, beside = torch.full_like(c.states, 7.0), torch.full_like(c.states, 7.0)
+    c.op.backward(c.q, c.k, c.v, c.lam, c.d_o, d_state_in=alone, **kw)
+    *_, want = R.linear_backward(c.wide(c.q, heads, dim_k), c.wide(c.k, kv_heads, dim_k), c.wide(c.v, kv_heads, dim_v), c.lam, lengths, c.scale, c.wide(c.d_o, heads, dim_v),
+                                 c.states, None, c.d_states)
+    assert off(alone, want) <= SUMS
+    dq, dk, dv = (c.space(c.rows, h * d, pad) for h, d in ((heads, dim_k), (kv_heads, dim_k), (kv_heads, dim_v)))
+    c.op.backward(c.q, c.k, c.v, c.lam, c.d_o, dq, dk, dv, d_state_in=beside, **kw)
+    assert off(alone, beside) <= SUMS
+    c.op.backward(c.q, c.k, c.v, c.lam, c.d_o, d_state_in=beside, **dict(kw, state_in=None, d_state_out=None))      # (linear in d_o and d_state_out; does not read state_in)
+    zero = torch.zeros_like(c.states)
+    *_, want = R.linear_backward(c.wide(c.q, heads, dim_k), c.wide(c.k, kv_heads, dim_k), c.wide(c.v, kv_heads, dim_v), c.lam, lengths, c.scale, c.wide(c.d_o, heads, dim_v),
+                                 zero, None, zero)
+    assert off(beside, want) <= SUMS
+
+
+@pytest.mark.parametrize("dtype,states", [("f32", True), ("f32", False), ("bf16", False)])
+@pytest.mark.parametrize("lengths", [[150], [700, 0, 30]])
+@pytest.mark.parametrize("heads,kv_heads,dim,pad", [(2, 2, 64, 0), (4, 2, 32, 8), (2, 1, 72, 3), (1, 1, 128, 0)])
+def test_linear_gradients_one_at_a_time_have_the_same_bits(dtype, states, lengths, heads, kv_heads, dim, pad):
+    """fp32, and bf16 where no state is asked for: the same launches, so the same order of sums (bf16 with d_state_in keeps more of the weighted rows, for all gradients of the call).
+    Forward: o with and without the state, in fp32."""
+    c = mixing(dtype, lengths, heads, kv_heads, dim, dim, pad, states=states, seed=6)
+    torch = c.torch
+    shapes = dict(dq=heads * dim, dk=kv_heads * dim, dv=kv_heads * dim)
+    kw = dict(starts=c.starts, state_in=c.states, d_state_out=c.d_states, workspace=c.ws(True))
+    every = {w: c.space(c.rows, n, pad) for w, n in shapes.items()}
+    ds = torch.full_like(c.states, 7.0) if states else None
+    c.op.backward(c.q, c.k, c.v, c.lam, c.d_o, **every, d_state_in=ds, **kw)
+    for which, n in shapes.items():
+        one = c.space(c.rows, n, pad)
+        c.op.backward(c.q, c.k, c.v, c.lam, c.d_o, **{which: one}, **kw)
+        assert torch.equal(one, every[which]), which
+    if states:
+        o, p, after = c.space(c.rows, heads * dim, pad), c.space(c.rows, heads * dim, pad), torch.empty_like(c.states)
+        c.op.forward(c.q, c.k, c.v, c.lam, o, starts=c.starts, state_in=c.states, state_out=after, workspace=c.ws())
+        c.op.forward(c.q, c.k, c.v, c.lam, p, starts=c.starts, state_in=c.states, workspace=c.ws())
+        assert torch.equal(o, p)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("dim_k,dim_v,pad", [(64, 96, 0), (96, 24, 8), (128, 256, 0), (250, 60, 1), (16, 192, 0), (32, 48, 0), (30, 34, 5), (128, 64, 1)])
 @pytest.mark.parametrize("lengths", [[90], [800, 0, 70]])
 def test_linear_gradients_of_keys_and_values_of_unlike_width(dtype, lengths, dim_k, dim_v, pad):
@@ -556,6 +606,76 @@ def test_gated_by_gates_that_are_all_but_open_or_closed(dtype, gate):
     op.forward(y, g, None, None, None, x_out=x)
     want = (sig if gate == "sigmoid" else v * sig) * u * ((u * u).mean(1, keepdim=True) + 1e-6).rsqrt()
     assert bool(((x.double() - want).abs() <= ((0 if dtype == "f32" else 2.0 ** -8) + (steps + 14) * 2.0 ** -23) * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gate", ["none", "column", "plain", "sigmoid", "silu"])
+def test_gated_gradients_of_one_column(dtype, gate):
+    """The norm of one column is its sign: a gradient through it is what is left of nearly equal terms, so each result is bounded by roundings of its terms, 2^-24 each (gates: 10 steps of
+    2^-23 with fp32, 36 with bf16 rows, as above), and by its own one."""
+    torch, ddg, kind, mk, space, g, gain_y, gain_x = gated_case(dtype, 37, 1, 0, gate, False)
+    rows = 37
+    y, x, d_out, d_x = mk(rows, 1, 0, 3.0), mk(rows, 1, 0, 2.0), mk(rows, 1), mk(rows, 1)
+    ry, rx = (y.float().square().mean(1) + 1e-5).rsqrt().reshape(rows, 1), (x.float().square().mean(1) + 1e-5).rsqrt()
+    op = ddg.GatedJoin(rows, 1, kind, eps=1e-5, gate=gate, scale=0.7, residual_scale=0.9)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    d_res, d_y, dgy, dgx = space(rows, 1), space(rows, 1), space(1, 1, dt=torch.float32), space(1, 1, dt=torch.float32)
+    d_gate = None if gate == "none" else space(1, 1, dt=torch.float32) if gate == "column" else space(rows, 1)
+    op.backward(y, ry, g, x, rx, gain_y, gain_x, d_out=d_out, d_x=d_x, d_residual=d_res, d_y=d_y, d_gate=d_gate, d_gain_y=dgy, d_gain_x=dgx, workspace=ws)
+    wr, wy, wg, wgy, wgx = R.gated_backward(y, ry, gate, g, x, rx, gain_y, gain_x, d_out, d_x, 0, 0.7, 0.9)
+    a, r, n = d_out.double(), rx.double().reshape(rows, 1), y.double() * ry.double()
+    xhat, w = x.double() * r, (d_out.double() * gain_x.double()).abs()
+    t = d_x.double().abs() + r * (w + xhat * xhat * w)                     # sizes of t's terms; ten roundings on the way
+    half, turn = 2.0 ** -24, 0.0 if dtype == "f32" else 2.0 ** -8
+    if gate == "none":
+        act = slope = torch.ones_like(t)
+    else:
+        act, v = R.gate(gate, g.double()), g.double()
+        s, rest = 1 / (1 + torch.exp(-v)), 1 / (1 + torch.exp(v))
+        slope = torch.ones_like(act) if gate in ("column", "plain") else s * rest if gate == "sigmoid" else s * (1 + v.abs() * rest)
+    gates = 0 if gate in ("none", "column", "plain") else 2 * (10 if dtype == "f32" else 36)
+    u = 0.7 * act.abs() * t
+    fits = lambda got, want, size, steps: bool(((got.double() - want).abs() <= half * steps * size + (turn + half) * want.abs()).all())  # noqa: E731
+    assert fits(d_res, wr, 0.9 * t, 12)
+    assert fits(d_y, wy, ry.double() * gain_y.double().abs() * u * (1 + n * n), 20 + gates)
+    sums = 37                                                                # (a sum of 37 terms in any order: a rounding of it for each)
+    assert fits(dgy, wgy, (u * n.abs()).sum(0), 16 + gates + sums) and fits(dgx, wgx, (a * xhat).abs().sum(0), 4 + sums)
+    size = 0.7 * t * (n * gain_y.double()).abs() * slope.abs()
+    if gate == "column":
+        assert fits(d_gate.reshape(1), wg.reshape(1), size.sum(0), 18 + sums)
+    elif gate != "none":
+        assert fits(d_gate, wg, size, 18 + gates)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,group,pad", [(1, 64, 8, 0), (33, 1024, 64, 0), (7, 520, 8, 3), (300, 2048, 128, 0), (5, 192, 64, 5), (4, 4104, 8, 0), (9, 1001, 0, 1), (600, 96, 32, 0)])
+@pytest.mark.parametrize("gate", ["none", "column", "plain", "sigmoid", "silu"])
+def test_gated_norm_without_a_join(dtype, rows, cols, group, pad, gate):
+    """The norm behind a block and its gate alone, as before a projection: no residual and no next norm; backward from the gradient of its result."""
+    torch, ddg, kind, mk, space, g, gain_y, _ = gated_case(dtype, rows, cols, pad, gate, False)
+    print(f"case gated norm alone {dtype} {rows}x{cols}+{pad} group {group} {gate}", flush=True)
+    ld, parts = cols + pad, cols // group if group else 1
+    y, d = mk(rows, cols, pad, 3.0), mk(rows, cols, pad)
+    x, ry = space(rows, cols, pad), space(rows, parts, dt=torch.float32)
+    op = ddg.GatedJoin(rows, cols, kind, eps=1e-5, gate=gate, group=group, ld_y=ld, ld_gate=ld, ld_x=ld)
+    op.forward(y, g, None, gain_y, None, x_out=x, rstd_y=ry)
+    wx, _, wry, _ = R.gated(y, gate, g, None, gain_y, None, 1e-5, group, 1.0, 1.0)
+    assert off(x, wx) <= ROUND[dtype] and off(ry, wry) <= SUMS and untouched(torch, x, pad)
+    d_y, dgy = space(rows, cols, pad), space(1, cols, dt=torch.float32)
+    d_gate = None if gate == "none" else space(1, cols, dt=torch.float32) if gate == "column" else space(rows, cols, pad)
+    ws = torch.full((op.workspace_bytes(),), 255, device="cuda", dtype=torch.uint8)
+    op.backward(y, ry, g, None, None, gain_y, None, d_x=d, d_y=d_y, d_gate=d_gate, d_gain_y=dgy, workspace=ws)
+    _, wy, wg, wgy, _ = R.gated_backward(y, ry, gate, g, None, None, gain_y, None, None, d, group, 1.0, 1.0)
+    assert off(d_y, wy) <= ROUND[dtype] and off(dgy, wgy) <= SUMS and untouched(torch, d_y, pad)
+    assert d_gate is None or off(d_gate, wg) <= (SUMS if gate == "column" else ROUND[dtype])
+    leaf = [y.double(), gain_y.double()] + ([] if g is None else [g.double()])
+    for t in leaf:
+        t.requires_grad_(True)
+    with torch.enable_grad():
+        out = R.gated(leaf[0], gate, leaf[2] if g is not None else None, None, leaf[1], None, 1e-5, group, 1.0, 1.0)[0]
+        grads = torch.autograd.grad((out * d.double()).sum(), leaf)           # the formulas by automatic differentiation, statistics and all
+    for got, want in zip((d_y, dgy, d_gate), grads):
+        assert off(got.reshape(want.shape), want) <= (ROUND[dtype] if got.dtype != torch.float32 else SUMS)
 
 
 @pytest.mark.parametrize("rows", [0, 1])
