@@ -822,3 +822,61 @@ def test_a_block_in_a_graph(dtype):
         assert turn or all(torch.equal(a, b) for a, b in zip(eager, first))
         for t in inputs[:5]:
             t.add_(0.25)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ragged_prompts_and_tokens_in_a_graph(dtype):
+    """A captured pass over ragged prompts, their gradients and a row of every sequence, replayed with other starts, slots and positions in the same tensors: the eager bits every time."""
+    torch, ddg, kind, t, gen, mk, space = setup(dtype, 4)
+    rows, heads, kv_heads, dim, count, pool = 900, 4, 2, 64, 6, 9
+    q, k, v, d_o = mk(rows, heads * dim), mk(rows, kv_heads * dim), mk(rows, kv_heads * dim), mk(rows, heads * dim)
+    lam = torch.tensor([-0.01, -0.2, 0.0, -1.0], device="cuda")
+    begin = torch.randn((pool, heads, dim, dim), device="cuda", generator=gen)
+    starts, slots = (torch.zeros(n, device="cuda", dtype=torch.int32) for n in (count + 1, count))
+    positions = torch.zeros(rows, device="cuda", dtype=torch.int32)
+    table = torch.from_numpy(ddg.Rotary(rows, heads, dim, kind).table().view("int64")).cuda()
+    need = ddg.LinearAttention(rows, heads, dim, dim, kind, sequences=count, kv_heads=kv_heads, slots=pool).workspace_bytes(True)
+    ws = torch.full((need,), 255, device="cuda", dtype=torch.uint8)
+
+    def run(stream):
+        mix = ddg.LinearAttention(rows, heads, dim, dim, kind, sequences=count, kv_heads=kv_heads, slots=pool, stream=stream)
+        one = ddg.LinearAttention(count, heads, dim, dim, kind, kv_heads=kv_heads, slots=pool, stream=stream)
+        o, tq, states = torch.zeros_like(d_o), torch.empty_like(q), torch.empty_like(begin)
+        dq, dk, dv, ds, token = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v), torch.zeros_like(begin), torch.empty((count, heads * dim), device="cuda", dtype=t)
+        states.copy_(begin)
+        ddg.Rotary(rows, heads, dim, kind, stream=stream)(q, tq, table, positions=positions)
+        mix.forward(tq, k, v, lam, o, starts=starts, slots=slots, state_in=states, state_out=states, workspace=ws)
+        mix.backward(tq, k, v, lam, d_o, dq, dk, dv, starts=starts, slots=slots, state_in=begin, d_state_in=ds, workspace=ws)
+        one.step(q[:count], k[:count], v[:count], lam, token, slots=slots, state_in=states, state_out=states)
+        return o, dq, dk, dv, ds, states, token
+
+    turns = [([0, 300, 300, 310, 700, 701, 900], [3, 0, 8, 1, -1, 5]), ([5, 6, 7, 8, 9, 10, 11], [0, 1, 2, 3, 4, 5]), ([0, 0, 0, 900, 900, 900, 900], [8, 7, 6, 5, 4, 3]),
+             ([100, 228, 420, 613, 614, 615, 890], [2, 9, 4, 6, 8, 0])]
+
+    def put(turn):
+        starts.copy_(torch.tensor(turns[turn][0], dtype=torch.int32))
+        slots.copy_(torch.tensor(turns[turn][1], dtype=torch.int32))
+        positions.copy_(torch.arange(rows, dtype=torch.int32) * (turn + 1) - 7)
+
+    put(0)
+    run(None)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        results = run(torch.cuda.current_stream().cuda_stream)
+    for turn in (0, 1, 2, 3, 0):
+        put(turn)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = run(None)
+        assert all(torch.equal(a, b) for a, b in zip(results, eager)), turn
+        begins, named = turns[turn]
+        lengths = [b - a for a, b in zip(begins, begins[1:])]
+        where = slice(begins[0], begins[-1])
+        wide = lambda x, h: x[where].reshape(-1, h, dim)  # noqa: E731
+        turned = R.rotary(q, heads, dim, dim, positions.tolist()).to(t)
+        want, _ = R.linear(wide(turned, heads), wide(k, kv_heads), wide(v, kv_heads), lam, lengths, dim ** -0.5, begin, named)
+        bound = MIX[dtype] if dtype == "f32" else 2 * MIX[dtype]                # (the turned row that is compared with is rounded from 64 bits: some round the other way)
+        assert off(results[0][where], want.reshape(-1, heads * dim)) <= bound
+        assert bool((results[0][:begins[0]] == 0).all()) and bool((results[0][begins[-1]:] == 0).all())
