@@ -5,15 +5,15 @@
 //   t = d_x + rstd_x (gain_x d_out - xhat c),  d_residual = residual_scale t,  d_u = scale act t,  d_gate = scale t u act',
 //   d_y = rstd_y (gain_y d_u - yhat mean(gain_y d_u yhat)),  d_gain_y = sum d_u yhat,  d_gain_x = sum d_out xhat.
 // Bound by memory: a row is held in registers, every operand is read once and every result written once, rounded once from 32 bits
-// (8192 x 2048 in bf16, a norm per 128 columns, silu: 35 us forward, 168 MB, 4.8 TB/s; 62 us backward, 268 MB, 4.3 TB/s).
+// (8192 x 2048 in bf16, a norm per 128 columns, silu: 35 us forward, 168 MB, 4.8 TB/s; 63 us backward, 268 MB, 4.2 TB/s).
 #include "ddg_mixing.h"
 #include "ddg_rows.h"
 
 namespace ddg {
 namespace {
 
-// A unit of 8 columns a lane. 16 waves have 128 registers a lane, which leaves none for the next row's operands (4096 x 8192 in bf16, backward: 116 us; 8 waves of two units, whose
-// registers do not fit, 177).
+// A unit of 8 columns a lane. 16 waves have 128 registers a lane, which leaves none for the next row's operands (4096 x 8192 in bf16, backward: 121 us; 8 waves of two units, whose
+// registers do not fit, 177). Backward only aligned bf16 rows without a column gate fit at all: the other seven forms spill 22 to 78 of a row's own (119 us with a column gate, 264 unaligned; fp32 319).
 constexpr int U = 1;
 
 // Sum over the `lanes` (a power of two) neighbouring lanes that share a norm, in each of them

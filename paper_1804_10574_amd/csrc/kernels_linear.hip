@@ -5,7 +5,7 @@
 // three matrix products of 64 rows for each of S's 64-column slices, 4 K V flops a row in the end where the sum over all pairs would take T (K + V).
 // A workgroup of four waves walks over a sequence (or a segment of one) for one head and one slice; S stays in its registers in 32 bits and goes to LDS once a chunk,
 // as the operand of the next product. One prompt of 16384 rows, 16 heads of 128, bf16: 135 us, of which the walk 90 (276 MB, 3.1 TB/s; vector, matrix and LDS
-// instructions take a third of its cycles each and overlap little), gradients of 8 sequences of 1024 rows 121 us. Where there are fewer sequences and heads than the chip holds, sequences are cut into segments: a pass that only adds up
+// instructions take a third of its cycles each and overlap little), gradients of 8 sequences of 1024 rows 118 us. Where there are fewer sequences and heads than the chip holds, sequences are cut into segments: a pass that only adds up
 // each segment's own state, a short scan over the segments, and the walk, which starts each segment from the state that the scan left.
 #include "ddg_mixing.h"
 #include "ddg_rows.h"
@@ -515,6 +515,8 @@ __device__ __forceinline__ void walk(const LinearArgs& g) {
 
 // TWO: jobs whose keys are much narrower than the launch's widest (the gradients' walks swap keys and values) walk in tiles of `narrower` columns (777 fp32 rows of 40 x 72: 25 us,
 // 29.5 in one width). A kernel of its own: the registers of a walk of 128 columns do not hold both (2 spilled, 3 % of it).
+// Two workgroups a compute unit leave 256 registers a lane, which hold every aligned bf16 walk of one width up to 128 columns but not all others (spilled: fp32 of 96 columns 9 at most on whole pieces
+// and 40 to 47 on rows that lie anywhere, the 777 rows among them; bf16 rows that lie anywhere 1 to 13). Of 256 columns fp32 walks spill 12 to 50 of the 512 that one workgroup leaves.
 constexpr int narrower(int DK) { return DK <= 64 ? 32 : DK <= 128 ? 64 : DK / 2; }
 template <typename T, int DK, int PLANES, bool VEC, bool SUM, bool TWO>
 __global__ __launch_bounds__(256, DK <= (sizeof(T) == 2 ? 128 : SUM ? 0 : 96) ? 2 : 1) void walk_kernel(LinearArgs g) {
@@ -746,9 +748,9 @@ template <typename T> hipError_t step_typed(const LinearStepArgs& given, hipStre
 
 }  // namespace
 
-// Two workgroups a compute unit are resident: fewer walks than that are cut, for as many (a prompt of 16384 rows, 16 heads of 128, bf16: 130 us in segments of 1024 rows, 140 of 512, 172
-// of 2048). A segment costs three passes over a state, so the shortest is three chunks (3010 ragged rows of 12 heads, 64 x 128: 37 us, 42 with two chunks, 41 with one; 72 uncut), of fp32,
-// whose chunks take longer, one (777 ragged rows, gradients: 46 us, 60 with two, 90 uncut). Nobody knows how long the longest of ragged sequences is: 2048 rows are the most.
+// Two workgroups a compute unit are resident: fewer walks than that are cut, for as many (a prompt of 16384 rows, 16 heads of 128, bf16: 134 us in segments of 1024 rows, 145 of 512, 170
+// of 2048). A segment costs three passes over a state, so the shortest is three chunks (3010 ragged rows of 12 heads, 64 x 128: 32 us, 36 with two chunks, 41 with one; 70 uncut), of fp32,
+// whose chunks take longer, one (777 ragged rows, gradients: 42 us, 58 with two, 90 uncut). Nobody knows how long the longest of ragged sequences is: 2048 rows are the most.
 int linear_segment(int rows, int sequences, int walks, bool ragged, int dtype) {
   const int length = ragged ? rows : rows / sequences, average = rows / sequences, least = dtype == BF16 ? 3 * CHUNK : CHUNK;
   const long have = (long)sequences * walks, most = have < 512 ? (512 + have - 1) / have : 1;     // segments of a sequence of average length
